@@ -244,7 +244,18 @@ typedef enum hero_kernel {
                                       models: with the row's own terms of dL/dhbar               */
   HERO_K_ROUTER_BWD_ROWS = 25,     /* RMSNorm and transition terms of dL/dhbar (bf16 models: of
                                       the two earlier states' gradients only); dL/deta           */
-  HERO_K_COUNT = 26
+  /* the ends of a training step (hero_final_norm .. hero_grad_clip) */
+  HERO_K_FINAL_NORM = 26,          /* x = RMSNorm(h) * norm_w                                     */
+  HERO_K_FINAL_NORM_BWD = 27,      /* dL/dh and dL/dnorm_w                                        */
+  HERO_K_LM_ROWS = 28,             /* the counted tokens compacted, their targets' logits         */
+  HERO_K_LM_LOGITS = 29,           /* exp(x W^T - ref) of one piece of the vocabulary and its sums */
+  HERO_K_LM_COMBINE = 30,          /* the rows' sums with one piece's                             */
+  HERO_K_LM_DX = 31,               /* the piece's share of dL/dx                                  */
+  HERO_K_LM_FINISH = 32,           /* loss, token losses, dL/dx                                   */
+  HERO_K_LM_DW = 33,               /* dL/dW, all pieces                                           */
+  HERO_K_GRAD_NORM = 34,           /* sums of squares over all tensors                            */
+  HERO_K_GRAD_CLIP = 35,           /* the tensors scaled                                          */
+  HERO_K_COUNT = 36
 } hero_kernel;
 
 /*
@@ -617,6 +628,109 @@ int hero_router_backward(const hero_dims *dims, int j, int T, const void *hbar, 
                          float eta, const float *dlogit, const hero_router_carry *carry, float *dhbar,
                          float *dhbar_prev1, float *dhbar_prev2, const hero_router_grads *grads, float *deta,
                          void *workspace, size_t workspace_bytes, void *stream);
+
+/* ---------------------------------------------------------------------------------------
+ * The ends of a training step around the routed stack (Sec. 3.3: the language-model loss, to which
+ * the penalty of Eq. 18 is added): h_out -> final norm -> loss and dL/dx -> norm backward -> the
+ * backwards above -> clipping.  The loss without gradients scores text.
+ * ------------------------------------------------------------------------------------- */
+
+/* The model's final norm, x = RMSNorm(h) * norm_w per token row; h, x [T][d], norm_w [d] in dims.dtype, eps
+ * dims.eps_norm.  x must not overlap h or norm_w.  d <= 32768 (HERO_E_UNSUPPORTED above). */
+int hero_final_norm(const hero_dims *dims, int T, const void *h, const void *norm_w, void *x, void *stream);
+
+/*
+ * Its backward: with r = 1/rms(h), u = norm_w * dx,
+ *   dh = r u - h r^3 <h, u> / d   [T][d] dims.dtype, rounded once
+ *   dnorm_w = sum over the tokens of dx * h * r   [d] fp32, overwritten; NULL: a frozen gain, and no
+ *             workspace is needed (NULL, 0).  Added in a fixed order.
+ * dh must not overlap h, dx or norm_w; the workspace must not overlap any argument.
+ */
+int hero_final_norm_backward_workspace_size(const hero_dims *dims, int T, size_t *bytes);
+int hero_final_norm_backward(const hero_dims *dims, int T, const void *h, const void *dx, const void *norm_w, void *dh,
+                             float *dnorm_w, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * LM head: w [vocab][d] (dims.dtype), and for dL/dx its transposed copy w_t [d][HERO_LM_HEAD_PITCH(vocab)], zero
+ * in the columns past vocab, which hero_lm_head_weights_make fills (once for a frozen head; after every
+ * update for a trained one).  w_t may be NULL for calls without dx.
+ */
+#define HERO_LM_HEAD_PITCH(vocab) (((vocab) + 63) / 64 * 64)
+
+typedef struct hero_lm_head {
+  const void *w, *w_t;
+} hero_lm_head;
+
+int hero_lm_head_weights_make(const hero_dims *dims, int vocab, const void *w, void *w_t, void *stream);
+
+typedef enum hero_loss_reduction {
+  HERO_LOSS_SUM = 0,
+  HERO_LOSS_MEAN = 1        /* over the counted tokens; 0 when there are none */
+} hero_loss_reduction;
+
+/* Outputs of hero_lm_loss (device, overwritten):
+ *   loss        [1] fp32            required
+ *   token_loss  [T] fp32            each token's -log p(target), unscaled; 0 where the token does not count; or NULL
+ *   dx          [T][d] dims.dtype   dL/dx, rounded once, zero rows where the token does not count; or NULL
+ *   dw          [vocab][d] dims.dtype   dL/dW, rounded once; or NULL (a frozen head) */
+typedef struct hero_lm_loss_out {
+  float *loss, *token_loss;
+  void *dx, *dw;
+} hero_lm_loss_out;
+
+/* Workspace bytes for hero_lm_loss with and without the two gradients (nonzero: wanted).  Host-only.  About
+ * 0.3 GiB, with dx 4 d bytes more per token (at most 8192 of them), with dw 2 d per token. */
+int hero_lm_loss_workspace_size(const hero_dims *dims, int vocab, int T, int with_dx, int with_dw, size_t *bytes);
+
+/*
+ * Softmax cross entropy of the LM head and its gradients, without keeping the logits:
+ *   token_loss_t = log sum_v exp(<x_t, W_v>) - <x_t, W_y>,  y = targets[t] (device [T] i32)
+ *   loss = scale * (sum, or mean over the counted tokens, of token_loss);  dx, dw its gradients.
+ * A token counts when 0 <= targets[t] < vocab; any other target leaves it out (its row of x is then not
+ * used, whatever it holds, and costs nothing).  The caller shifts the targets (token t's is the token at t + 1).
+ * The vocabulary is taken in pieces whose exponentials live in the workspace.  Products are bf16 x bf16 with
+ * fp32 accumulation for a bf16 model, where exp(logit - reference) passes through memory in bf16 on its way to
+ * dx, and p - [v = y] to dw (fp32 otherwise); losses, sums and the target's own share are fp32 throughout.  A
+ * logit that is not finite leaves no finite loss or gradient of its token.
+ * Every sum runs in a fixed order.
+ * Errors: HERO_E_DIM (vocab, T), HERO_E_UNSUPPORTED (vocab above 4194240, T above 2^24; bf16: vocab below 65, or
+ * x, w_t, or 131072 rows of w spanning 4 GiB or more), HERO_E_RANGE (reduction, scale not finite), HERO_E_NULL (w_t with dx),
+ * HERO_E_ALIGN, HERO_E_ALIAS, HERO_E_WORKSPACE, HERO_E_DEVICE, HERO_E_LAUNCH.
+ */
+int hero_lm_loss(const hero_dims *dims, int vocab, int T, const void *x, const hero_lm_head *head,
+                 const int32_t *targets, int reduction, float scale, const hero_lm_loss_out *out, void *workspace,
+                 size_t workspace_bytes, void *stream);
+
+/*
+ * One gradient tensor of a list (HOST array): count elements of dtype at grad (device, aligned to its elements
+ * only: views are fine), contiguous; out (hero_grad_clip) is grad itself or disjoint from every other range of the call.
+ * count may be 0.  At most HERO_GRAD_MAX_TENSORS tensors of at most 2^36 elements (HERO_E_UNSUPPORTED above).
+ */
+#define HERO_GRAD_MAX_TENSORS 4096
+
+typedef struct hero_grad_tensor {
+  const void *grad;
+  void *out;
+  size_t count;
+  int dtype;
+} hero_grad_tensor;
+
+/* Workspace bytes of the two calls below.  Host-only; checks the list (out is not read). */
+int hero_grad_norm_workspace_size(int n_tensors, const hero_grad_tensor *tensors, size_t *bytes);
+
+/* norm[0] (device fp32) = sqrt of the sum of squares over all tensors, squared and added in 64 bits and in a fixed
+ * order.  out is not read. */
+int hero_grad_norm(int n_tensors, const hero_grad_tensor *tensors, float *norm, void *workspace, size_t workspace_bytes,
+                   void *stream);
+
+/*
+ * norm[0] as above, and out = grad * min(1, max_norm / norm) in each tensor's dtype, rounded once.  max_norm >= 0
+ * (HERO_E_RANGE; +inf is allowed).  Where the factor is 1, a tensor scaled in place is not touched.  A norm that is
+ * NaN makes every element NaN, an infinite one zero or NaN.  The list travels with the launches: nothing of it is read
+ * after the call returns, and a captured call replays with the same pointers.
+ */
+int hero_grad_clip(int n_tensors, const hero_grad_tensor *tensors, float max_norm, float *norm, void *workspace,
+                   size_t workspace_bytes, void *stream);
 
 #ifdef __cplusplus
 }

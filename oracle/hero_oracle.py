@@ -797,6 +797,53 @@ def skip_penalty(gates, batch, seq, alpha=1.0):
     return value, grad.reshape(gates.shape)
 
 
+def rmsnorm_gain_grad(h, eps_norm, du):
+    """dL/dgain of u = h r gain, summed over the token rows."""
+    h = np.asarray(h, dtype=f64)
+    return np.sum(du * h / np.sqrt(np.mean(h * h, axis=-1, keepdims=True) + eps_norm), axis=0)
+
+
+@dataclasses.dataclass
+class LmLoss:
+    loss: float
+    token_loss: np.ndarray   # [T], 0 where the token does not count
+    dx: np.ndarray           # [T][d]
+    dw: np.ndarray           # [vocab][d]
+
+
+def lm_loss(x, w, targets, scale=1.0, mean=True):
+    """Softmax cross entropy of the logits x w^T (the language-model loss of Sec. 3.3) and its gradients.
+    A token counts when its target is a row of w; the mean is over those, 0 without any."""
+    x, w, y = np.asarray(x, dtype=f64), np.asarray(w, dtype=f64), np.asarray(targets)
+    rows = np.flatnonzero((y >= 0) & (y < w.shape[0]))
+    token, dx = np.zeros(len(y)), np.zeros_like(x)
+    if len(rows) == 0:
+        return LmLoss(0.0, token, dx, np.zeros_like(w))
+    unit = scale / len(rows) if mean else scale
+    xr, at = x[rows], (np.arange(len(rows)), y[rows])
+    p = xr @ w.T
+    p -= p[at][:, None]                      # relative to the target's logit
+    top = np.maximum(p.max(axis=1, keepdims=True), 0.0)
+    p = np.exp(p - top)
+    p[at] = 0.0
+    others, own = p.sum(axis=1), np.exp(-top[:, 0])
+    near = top[:, 0] < 30.0                  # log(1 + S) without a cancellation
+    token[rows] = np.where(near, np.log1p(others * np.exp(np.minimum(top[:, 0], 30.0))),
+                           np.log(others + own) + top[:, 0])
+    p /= (others + own)[:, None]
+    p[at] = -others / (others + own)
+    p *= unit
+    dx[rows] = p @ w
+    return LmLoss(float(token.sum() * unit), token, dx, p.T @ xr)
+
+
+def grad_clip(grads, max_norm):
+    """Global norm of a list of arrays, and each scaled by min(1, max_norm / norm)."""
+    norm = math.sqrt(sum(float(np.sum(np.square(np.asarray(g, dtype=f64)))) for g in grads))
+    c = 1.0 if norm <= max_norm else max_norm / norm
+    return norm, [np.asarray(g, dtype=f64) * c for g in grads]
+
+
 # ---------------------------------------------------------------------------
 # Training side, continued: gradients reach the router through the gate scaling
 # (Sec. 3.1, the remark after eq:ffn_route), and the router's encoders, depth memory and

@@ -1679,3 +1679,428 @@ int hero_router_backward(const hero_dims* dims, int j, int T, const void* hbar, 
   e = join_side(e);
   return e == hipSuccess ? HERO_OK : HERO_E_LAUNCH;
 }
+
+// ---------------------------------------------------------------------------
+// The ends of a training step: final norm, language-model loss, gradient clipping
+// ---------------------------------------------------------------------------
+namespace {
+
+struct Region {
+  const void* p;
+  size_t bytes;
+};
+
+// whether a written region overlaps another written one or a read one
+template <size_t W, size_t R>
+bool any_overlap(const Region (&written)[W], const Region (&read)[R]) {
+  for (size_t i = 0; i < W; ++i) {
+    for (size_t j = i + 1; j < W; ++j)
+      if (overlap(written[i].p, written[i].bytes, written[j].p, written[j].bytes)) return true;
+    for (size_t j = 0; j < R; ++j)
+      if (overlap(written[i].p, written[i].bytes, read[j].p, read[j].bytes)) return true;
+  }
+  return false;
+}
+
+constexpr int kLmChunk = 8192;               // rows of one chunk
+constexpr size_t kLmPieceBytes = 256u << 20; // of e (or of dW's g) for one chunk and piece: the last-level cache's size
+constexpr int kLmVocabMax = 65535 * 64;      // grid limit of the head's transpose
+constexpr int kLmVocabMin = 65;              // bf16: the products take K in at least two k-tiles
+constexpr int kLmHeadRows = 1 << 17;         // head rows of a product, which addresses them with 32 bits
+
+struct LmLayout {
+  int chunk, n_chunks;       // rows of a chunk, chunks of T rows
+  int cols, pieces, pitch;   // columns of a piece (the last takes the rest), widest piece's pitch
+  int slices;                // K slices of the dx products
+  int g_cols, g_pitch, g_ldl;
+  size_t idx, inv, tgt, counts, lt, ref, sum, alpha, e, part, acc, lse, own, g, xT, logits, total;
+};
+
+int lm_piece_cols(const LmLayout& L, int vocab, int k) { return k == L.pieces - 1 ? vocab - k * L.cols : L.cols; }
+
+LmLayout lm_layout_of(const hero_dims& d, int vocab, int T, bool dx, bool dw) {
+  LmLayout L{};
+  size_t off = 0;
+  auto take = [&](size_t bytes) {
+    const size_t o = off;
+    off = align_up(off + bytes);
+    return o;
+  };
+  const size_t t = static_cast<size_t>(T), es = esize(d.dtype);
+  const bool mfma = d.dtype == HERO_BF16;
+  auto up64 = [](int n) { return (n + 63) / 64 * 64; };
+  // whole tiles of 256 columns whose rows fit the piece; the loss alone keeps no e in bf16, only the sums
+  auto fit = [&](size_t rows) {
+    const size_t c = kLmPieceBytes / (es * rows) / 256 * 256;
+    const size_t most = std::min<size_t>((static_cast<size_t>(vocab) + 255) / 256 * 256, kLmHeadRows - 256);
+    return static_cast<int>(std::min(std::max<size_t>(c, 256), most));
+  };
+  L.chunk = std::min(T, kLmChunk);
+  L.n_chunks = (T + L.chunk - 1) / L.chunk;
+  L.cols = fit(static_cast<size_t>(L.chunk));
+  L.pieces = std::max(1, (vocab - 127 + L.cols - 1) / L.cols);   // no piece of less than two k-tiles
+  const int last = vocab - (L.pieces - 1) * L.cols, widest = L.pieces > 1 ? std::max(L.cols, last) : last;
+  L.pitch = up64(widest);
+  L.slices = mfma && dx ? hero::lm_dx_slices(L.chunk, d.d, up64(L.pieces > 1 ? std::min(L.cols, last) : last)) : 1;
+  L.idx = take(t * 4);
+  L.inv = take(t * 4);
+  L.tgt = take(t * 4);
+  L.counts = take((1 + static_cast<size_t>(L.n_chunks)) * 4);
+  L.lt = take(t * 4);
+  L.ref = take(t * 4);
+  L.sum = take(t * 4);
+  L.alpha = take(t * 4);
+  const size_t c = static_cast<size_t>(L.chunk);
+  L.e = take(dx || !mfma ? c * L.pitch * es : 0);
+  L.part = take(mfma ? c * hero::lm_parts(widest) * 8 : 0);
+  L.acc = take(dx ? static_cast<size_t>(L.slices) * c * d.d * 4 : 0);
+  L.g_pitch = std::max(128, up64(T));
+  L.g_cols = fit(static_cast<size_t>(L.g_pitch));
+  L.g_ldl = std::min(L.g_cols, up64(vocab));
+  L.lse = take(dw ? t * 4 : 0);
+  L.own = take(dw ? t * 4 : 0);
+  L.g = take(dw ? static_cast<size_t>(std::min(L.g_cols, vocab)) * L.g_pitch * es : 0);
+  L.xT = take(dw ? static_cast<size_t>(d.d) * L.g_pitch * es : 0);
+  L.logits = take(dw && !mfma ? t * L.g_ldl * 4 : 0);
+  L.total = off;
+  return L;
+}
+
+int check_lm(const hero_dims* dims, int vocab, int T, bool dx, bool dw) {
+  const int st = check_dims(dims);
+  if (st != HERO_OK) return st;
+  if (vocab <= 0 || T <= 0) return HERO_E_DIM;
+  if (vocab > kLmVocabMax || T > (1 << 24)) return HERO_E_UNSUPPORTED;
+  if (dims->dtype != HERO_BF16) return HERO_OK;
+  const long long d = dims->d;
+  if (vocab < kLmVocabMin || T * d * 2 >= kGemmSpan || 256 * d * 2 >= kGemmSpan) return HERO_E_UNSUPPORTED;
+  if (dx && HERO_LM_HEAD_PITCH(static_cast<long long>(vocab)) * d * 2 >= kGemmSpan) return HERO_E_UNSUPPORTED;
+  // a piece's head rows, and x transposed
+  if (std::min(vocab, kLmHeadRows) * d * 2 >= kGemmSpan || (dw && (T + 128LL) * d * 2 >= kGemmSpan)) return HERO_E_UNSUPPORTED;
+  return HERO_OK;
+}
+
+}  // namespace
+
+int hero_final_norm(const hero_dims* dims, int T, const void* h, const void* norm_w, void* x, void* stream) {
+  int st = check_dims(dims);
+  if (st != HERO_OK) return st;
+  if (T <= 0) return HERO_E_DIM;
+  if (dims->d > hero::kNormWidest) return HERO_E_UNSUPPORTED;
+  if (!h || !norm_w || !x) return HERO_E_NULL;
+  if (!aligned16(h) || !aligned16(norm_w) || !aligned16(x)) return HERO_E_ALIGN;
+  const size_t wb = static_cast<size_t>(dims->d) * esize(dims->dtype), hb = wb * T;
+  const Region written[] = {{x, hb}}, read[] = {{h, hb}, {norm_w, wb}};
+  if (any_overlap(written, read)) return HERO_E_ALIAS;
+  if ((st = check_device()) != HERO_OK) return st;
+  const hipStream_t s = static_cast<hipStream_t>(stream);
+  const hipError_t e = timed(HERO_K_FINAL_NORM, s, [&] {
+    return hero::launch_final_norm(dims->dtype, h, norm_w, T, dims->d, dims->eps_norm, x, s);
+  });
+  return e == hipSuccess ? HERO_OK : HERO_E_LAUNCH;
+}
+
+int hero_final_norm_backward_workspace_size(const hero_dims* dims, int T, size_t* bytes) {
+  if (!bytes) return HERO_E_NULL;
+  const int st = check_dims(dims);
+  if (st != HERO_OK) return st;
+  if (T <= 0) return HERO_E_DIM;
+  if (dims->d > hero::kNormWidest) return HERO_E_UNSUPPORTED;
+  *bytes = align_up(static_cast<size_t>(hero::final_norm_bwd_groups(T, dims->d)) * dims->d * 4);
+  return HERO_OK;
+}
+
+int hero_final_norm_backward(const hero_dims* dims, int T, const void* h, const void* dx, const void* norm_w, void* dh,
+                             float* dnorm_w, void* workspace, size_t workspace_bytes, void* stream) {
+  size_t need = 0;
+  int st = hero_final_norm_backward_workspace_size(dims, T, &need);
+  if (st != HERO_OK) return st;
+  if (!h || !dx || !norm_w || !dh) return HERO_E_NULL;
+  const void* al[] = {h, dx, norm_w, dh, dnorm_w, workspace};
+  for (const void* p : al)
+    if (p && !aligned16(p)) return HERO_E_ALIGN;
+  if (dnorm_w && (!workspace || workspace_bytes < need)) return HERO_E_WORKSPACE;
+  const size_t wb = static_cast<size_t>(dims->d) * esize(dims->dtype), hb = wb * T;
+  const Region written[] = {{dh, hb}, {dnorm_w, static_cast<size_t>(dims->d) * 4}, {dnorm_w ? workspace : nullptr, need}};
+  const Region read[] = {{h, hb}, {dx, hb}, {norm_w, wb}};
+  if (any_overlap(written, read)) return HERO_E_ALIAS;
+  if ((st = check_device()) != HERO_OK) return st;
+  const hipStream_t s = static_cast<hipStream_t>(stream);
+  const hipError_t e = timed(HERO_K_FINAL_NORM_BWD, s, [&] {
+    return hero::launch_final_norm_bwd(dims->dtype, h, dx, norm_w, T, dims->d, dims->eps_norm, dh, dnorm_w,
+                                       static_cast<float*>(workspace), s);
+  });
+  return e == hipSuccess ? HERO_OK : HERO_E_LAUNCH;
+}
+
+int hero_lm_head_weights_make(const hero_dims* dims, int vocab, const void* w, void* w_t, void* stream) {
+  int st = check_lm(dims, vocab, 1, true, false);
+  if (st != HERO_OK) return st;
+  if (!w || !w_t) return HERO_E_NULL;
+  if (!aligned16(w) || !aligned16(w_t)) return HERO_E_ALIGN;
+  const size_t es = esize(dims->dtype), d = static_cast<size_t>(dims->d);
+  const int pitch = HERO_LM_HEAD_PITCH(vocab);
+  if (overlap(w_t, d * pitch * es, w, d * vocab * es)) return HERO_E_ALIAS;
+  if ((st = check_device()) != HERO_OK) return st;
+  return hero::launch_transpose(dims->dtype, w, vocab, dims->d, dims->d, w_t, pitch, pitch,
+                                static_cast<hipStream_t>(stream)) == hipSuccess
+             ? HERO_OK
+             : HERO_E_LAUNCH;
+}
+
+int hero_lm_loss_workspace_size(const hero_dims* dims, int vocab, int T, int with_dx, int with_dw, size_t* bytes) {
+  if (!bytes) return HERO_E_NULL;
+  const int st = check_lm(dims, vocab, T, with_dx != 0, with_dw != 0);
+  if (st != HERO_OK) return st;
+  *bytes = lm_layout_of(*dims, vocab, T, with_dx != 0, with_dw != 0).total;
+  return HERO_OK;
+}
+
+int hero_lm_loss(const hero_dims* dims, int vocab, int T, const void* x, const hero_lm_head* head, const int32_t* targets,
+                 int reduction, float scale, const hero_lm_loss_out* out, void* workspace, size_t workspace_bytes,
+                 void* stream) {
+  if (!out) return HERO_E_NULL;
+  const bool dx = out->dx != nullptr, dw = out->dw != nullptr;
+  int st = check_lm(dims, vocab, T, dx, dw);
+  if (st != HERO_OK) return st;
+  if (reduction != HERO_LOSS_SUM && reduction != HERO_LOSS_MEAN) return HERO_E_RANGE;
+  if (!(scale - scale == 0.f)) return HERO_E_RANGE;
+  if (!x || !head || !head->w || !targets || !out->loss || (dx && !head->w_t)) return HERO_E_NULL;
+  const void* al[] = {x, head->w, dx ? head->w_t : nullptr, targets, out->loss, out->token_loss, out->dx, out->dw, workspace};
+  for (const void* p : al)
+    if (p && !aligned16(p)) return HERO_E_ALIGN;
+  const hero_dims& D = *dims;
+  const LmLayout L = lm_layout_of(D, vocab, T, dx, dw);
+  if (!workspace || workspace_bytes < L.total) return HERO_E_WORKSPACE;
+  const size_t es = esize(D.dtype), xb = static_cast<size_t>(T) * D.d * es, wb = static_cast<size_t>(vocab) * D.d * es;
+  const int pitch = HERO_LM_HEAD_PITCH(vocab);
+  const Region written[] = {{out->loss, 4}, {out->token_loss, static_cast<size_t>(T) * 4}, {out->dx, xb}, {out->dw, wb},
+                            {workspace, L.total}};
+  const Region read[] = {{x, xb}, {head->w, wb}, {dx ? head->w_t : nullptr, static_cast<size_t>(D.d) * pitch * es},
+                         {targets, static_cast<size_t>(T) * 4}};
+  if (any_overlap(written, read)) return HERO_E_ALIAS;
+  if ((st = check_device()) != HERO_OK) return st;
+
+  const hipStream_t s = static_cast<hipStream_t>(stream);
+  unsigned char* ws = static_cast<unsigned char*>(workspace);
+  hero::LmRows a{};
+  a.dtype = D.dtype;
+  a.T = T;
+  a.d = D.d;
+  a.vocab = vocab;
+  a.x = x;
+  a.w = head->w;
+  a.targets = targets;
+  a.idx = reinterpret_cast<int*>(ws + L.idx);
+  a.inv = reinterpret_cast<int*>(ws + L.inv);
+  a.tgt = reinterpret_cast<int*>(ws + L.tgt);
+  a.counts = reinterpret_cast<int*>(ws + L.counts);
+  a.lt = reinterpret_cast<float*>(ws + L.lt);
+  a.ref = reinterpret_cast<float*>(ws + L.ref);
+  a.sum = reinterpret_cast<float*>(ws + L.sum);
+  a.alpha = reinterpret_cast<float*>(ws + L.alpha);
+  const bool mfma = D.dtype == HERO_BF16, mean = reduction == HERO_LOSS_MEAN;
+  hipError_t e = timed(HERO_K_LM_ROWS, s, [&] {
+    const hipError_t y = hero::launch_lm_rows(a, L.chunk, L.n_chunks, s);
+    return y == hipSuccess ? hero::launch_lm_targets(a, s) : y;
+  });
+  hero::LmFinish f{};
+  f.scale = scale;
+  f.mean = mean;
+  f.loss = out->loss;
+  f.token_loss = out->token_loss;
+  f.dx = out->dx;
+  f.lse = dw ? reinterpret_cast<float*>(ws + L.lse) : nullptr;
+  f.own = dw ? reinterpret_cast<float*>(ws + L.own) : nullptr;
+  f.acc = reinterpret_cast<float*>(ws + L.acc);
+  f.slices = L.slices;
+  for (int c = 0; c < L.n_chunks && e == hipSuccess; ++c) {
+    hero::LmPiece p{};
+    p.m0 = c * L.chunk;
+    p.rows_max = std::min(L.chunk, T - p.m0);
+    p.count = a.counts + 1 + c;
+    p.e = dx || !mfma ? ws + L.e : nullptr;
+    p.part = reinterpret_cast<float2*>(ws + L.part);
+    p.acc = reinterpret_cast<float*>(ws + L.acc);
+    p.slices = L.slices;
+    for (int k = 0; k < L.pieces && e == hipSuccess; ++k) {
+      p.v0 = k * L.cols;
+      p.cols = lm_piece_cols(L, vocab, k);
+      p.pitch = (p.cols + 63) / 64 * 64;
+      p.first = k == 0;
+      e = timed(HERO_K_LM_LOGITS, s, [&] { return hero::launch_lm_logits(a, p, s); });
+      if (e == hipSuccess) e = timed(HERO_K_LM_COMBINE, s, [&] { return hero::launch_lm_combine(a, p, s); });
+      if (e == hipSuccess && dx) e = timed(HERO_K_LM_DX, s, [&] { return hero::launch_lm_dx(a, p, head->w_t, pitch, s); });
+    }
+    f.last = c == L.n_chunks - 1;
+    if (!dx && !f.last) continue;
+    f.m0 = dx ? p.m0 : 0;
+    f.chunk = dx ? p.rows_max : T;
+    if (e == hipSuccess) e = timed(HERO_K_LM_FINISH, s, [&] { return hero::launch_lm_finish(a, f, s); });
+  }
+  if (e == hipSuccess && dw)
+    e = timed(HERO_K_LM_DW, s, [&] {
+      void *g = ws + L.g, *xT = ws + L.xT;
+      hipError_t y = hero::launch_lm_xT(a, xT, L.g_pitch, s);
+      for (int v0 = 0; v0 < vocab && y == hipSuccess; v0 += L.g_cols) {
+        const int cols = std::min(L.g_cols, vocab - v0);
+        if (mfma) {
+          y = hero::launch_lm_g(a, v0, cols, f.lse, f.own, g, L.g_pitch, s);
+        } else {
+          float* logits = reinterpret_cast<float*>(ws + L.logits);
+          hero::LmPiece p{};
+          p.rows_max = T;
+          p.v0 = v0;
+          p.cols = cols;
+          p.pitch = L.g_ldl;
+          p.count = a.counts;
+          p.e = logits;
+          y = hero::launch_lm_logits(a, p, s);
+          if (y == hipSuccess)
+            y = hero::launch_lm_g_f32(a, v0, cols, f.lse, f.own, logits, L.g_ldl, scale, mean, static_cast<float*>(g),
+                                      L.g_pitch, s);
+        }
+        if (y == hipSuccess) y = hero::launch_lm_dw(a, v0, cols, g, xT, L.g_pitch, scale, mean, out->dw, s);
+      }
+      return y;
+    });
+  return e == hipSuccess ? HERO_OK : HERO_E_LAUNCH;
+}
+
+// ---------------------------------------------------------------------------
+namespace {
+
+constexpr int kGradGroups = 2048;   // workgroups over all tensors, and so partial sums of the norm
+
+struct GradPlan {
+  int launches, groups;   // tables, workgroups (at most) of each
+  size_t bytes;
+};
+
+GradPlan grad_plan_of(int n) {
+  GradPlan p{};
+  p.launches = (n + hero::kGradTensors - 1) / hero::kGradTensors;
+  p.groups = std::max(64, kGradGroups / p.launches);
+  p.bytes = align_up(static_cast<size_t>(p.launches) * p.groups * sizeof(double));
+  return p;
+}
+
+int check_grads(int n, const hero_grad_tensor* g, bool clip) {
+  if (n <= 0) return HERO_E_DIM;
+  if (n > HERO_GRAD_MAX_TENSORS) return HERO_E_UNSUPPORTED;
+  if (!g) return HERO_E_NULL;
+  for (int i = 0; i < n; ++i) {
+    if (g[i].dtype != HERO_F32 && g[i].dtype != HERO_BF16) return HERO_E_DTYPE;
+    if (g[i].count == 0) continue;
+    if (g[i].count > (1ull << 36)) return HERO_E_UNSUPPORTED;
+    if (!g[i].grad || (clip && !g[i].out)) return HERO_E_NULL;
+    const uintptr_t m = esize(g[i].dtype) - 1;
+    if ((reinterpret_cast<uintptr_t>(g[i].grad) & m) || (clip && (reinterpret_cast<uintptr_t>(g[i].out) & m)))
+      return HERO_E_ALIGN;
+  }
+  return HERO_OK;
+}
+
+// whether a written range meets any other range; sorted by address, so that many tensors stay cheap
+bool grads_overlap(int n, const hero_grad_tensor* g, bool clip, const void* norm, const void* ws, size_t ws_bytes) {
+  struct Range {
+    uintptr_t a, b;
+    bool write;
+  };
+  Range r[2 * HERO_GRAD_MAX_TENSORS + 2];   // no allocation: nothing may throw here
+  int m = 0;
+  auto put = [&](const void* p, size_t bytes, bool write) {
+    const uintptr_t a = reinterpret_cast<uintptr_t>(p);
+    r[m++] = {a, a + bytes, write};
+  };
+  put(norm, 4, true);
+  put(ws, ws_bytes, true);
+  for (int i = 0; i < n; ++i) {
+    if (g[i].count == 0) continue;
+    const size_t bytes = g[i].count * esize(g[i].dtype);
+    const bool in_place = clip && g[i].out == g[i].grad;
+    if (!in_place) put(g[i].grad, bytes, false);
+    if (clip) put(g[i].out, bytes, true);
+  }
+  std::sort(r, r + m, [](const Range& x, const Range& y) { return x.a < y.a; });
+  uintptr_t end = 0, written = 0;
+  for (int i = 0; i < m; ++i) {
+    if (r[i].a < (r[i].write ? end : written)) return true;
+    end = std::max(end, r[i].b);
+    if (r[i].write) written = std::max(written, r[i].b);
+  }
+  return false;
+}
+
+// the norm's partial sums, and with clip the scaled gradients
+int run_grads(int n, const hero_grad_tensor* g, bool clip, float max_norm, float* norm, void* workspace,
+              size_t workspace_bytes, void* stream) {
+  int st = check_grads(n, g, clip);
+  if (st != HERO_OK) return st;
+  if (clip && !(max_norm >= 0.f)) return HERO_E_RANGE;
+  if (!norm) return HERO_E_NULL;
+  if (!aligned16(norm) || (workspace && !aligned16(workspace))) return HERO_E_ALIGN;
+  const GradPlan p = grad_plan_of(n);
+  if (!workspace || workspace_bytes < p.bytes) return HERO_E_WORKSPACE;
+  if (grads_overlap(n, g, clip, norm, workspace, p.bytes)) return HERO_E_ALIAS;
+  if ((st = check_device()) != HERO_OK) return st;
+  const hipStream_t s = static_cast<hipStream_t>(stream);
+  double* part = static_cast<double*>(workspace);
+  // the i-th table: its tensors, the workgroups it takes, and where their partial sums lie
+  hero::GradTable tab;
+  auto table = [&](int i) {
+    uint64_t chunks = 0;
+    tab.n = std::min(hero::kGradTensors, n - i * hero::kGradTensors);
+    for (int k = 0; k < tab.n; ++k) {
+      const hero_grad_tensor& t = g[i * hero::kGradTensors + k];
+      tab.grad[k] = t.grad;
+      tab.out[k] = clip ? t.out : nullptr;
+      tab.count[k] = t.count;
+      tab.bf16[k] = t.dtype == HERO_BF16;
+      tab.chunk0[k] = static_cast<uint32_t>(chunks);
+      chunks += (t.count + hero::kGradChunk - 1) / hero::kGradChunk;
+    }
+    tab.chunk0[tab.n] = static_cast<uint32_t>(chunks);
+    return chunks;
+  };
+  auto groups = [&](uint64_t chunks) { return static_cast<int>(std::max<uint64_t>(1, std::min<uint64_t>(chunks, p.groups))); };
+  int total = 0;
+  hipError_t e = timed(HERO_K_GRAD_NORM, s, [&] {
+    hipError_t y = hipSuccess;
+    for (int i = 0; i < p.launches && y == hipSuccess; ++i) {
+      const uint64_t c = table(i);
+      y = hero::launch_grad_norm(tab, groups(c), part + total, s);
+      total += groups(c);
+    }
+    return y == hipSuccess && !clip ? hero::launch_grad_norm_finish(part, total, norm, s) : y;
+  });
+  if (e == hipSuccess && clip)
+    e = timed(HERO_K_GRAD_CLIP, s, [&] {
+      hipError_t y = hipSuccess;
+      for (int i = 0; i < p.launches && y == hipSuccess; ++i)
+        y = hero::launch_grad_clip(tab, groups(p.launches == 1 ? tab.chunk0[tab.n] : table(i)), part, total, max_norm,
+                                   i == 0 ? norm : nullptr, s);
+      return y;
+    });
+  return e == hipSuccess ? HERO_OK : HERO_E_LAUNCH;
+}
+
+}  // namespace
+
+int hero_grad_norm_workspace_size(int n_tensors, const hero_grad_tensor* tensors, size_t* bytes) {
+  if (!bytes) return HERO_E_NULL;
+  const int st = check_grads(n_tensors, tensors, false);
+  if (st != HERO_OK) return st;
+  *bytes = grad_plan_of(n_tensors).bytes;
+  return HERO_OK;
+}
+
+int hero_grad_norm(int n_tensors, const hero_grad_tensor* tensors, float* norm, void* workspace, size_t workspace_bytes,
+                   void* stream) {
+  return run_grads(n_tensors, tensors, false, 0.f, norm, workspace, workspace_bytes, stream);
+}
+
+int hero_grad_clip(int n_tensors, const hero_grad_tensor* tensors, float max_norm, float* norm, void* workspace,
+                   size_t workspace_bytes, void* stream) {
+  return run_grads(n_tensors, tensors, true, max_norm, norm, workspace, workspace_bytes, stream);
+}

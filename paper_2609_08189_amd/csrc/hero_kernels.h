@@ -374,4 +374,92 @@ hipError_t launch_to_f32_transpose(int dtype, const void* in, int R, int C, int 
 hipError_t launch_skip_penalty(const float* gates, int L_R, int batch, int seq, float alpha, float* loss,
                                float* dgates, hipStream_t s);
 
+// Final RMSNorm and its backward (k_norm.hip); part: final_norm_bwd_groups(T, d) d floats, used when
+// dnorm_w is wanted.  d <= kNormWidest.
+constexpr int kNormWidest = 32768;
+int final_norm_bwd_groups(int T, int d);
+hipError_t launch_final_norm(int dtype, const void* h, const void* norm_w, int T, int d, float eps, void* x,
+                             hipStream_t s);
+hipError_t launch_final_norm_bwd(int dtype, const void* h, const void* dx, const void* norm_w, int T, int d, float eps,
+                                 void* dh, float* dnorm_w, float* part, hipStream_t s);
+
+// Global gradient norm and clipping (k_grad.hip).  A table goes to the kernels by value, so that a
+// captured graph holds it and nothing is copied: kGradTensors tensors a launch.
+constexpr int kGradTensors = 96, kGradChunk = 8192;
+struct GradTable {
+  const void* grad[kGradTensors];
+  void* out[kGradTensors];
+  uint64_t count[kGradTensors];
+  uint32_t chunk0[kGradTensors + 1];   // chunks of kGradChunk elements before tensor i
+  uint8_t bf16[kGradTensors];
+  int n;
+};
+hipError_t launch_grad_norm(const GradTable& tab, int groups, double* part, hipStream_t s);
+hipError_t launch_grad_norm_finish(const double* part, int n, float* norm, hipStream_t s);
+// norm may be null (a launch of a later table)
+hipError_t launch_grad_clip(const GradTable& tab, int groups, const double* part, int n, float max_norm, float* norm,
+                            hipStream_t s);
+
+// Language-model loss (k_lm_loss.hip, its products in k_gemm.hip).  Counted tokens are compacted: row
+// m < counts[0] is token idx[m].
+struct LmRows {
+  int dtype, T, d, vocab;
+  const void *x, *w;         // [T][d], [vocab][d]
+  const int* targets;        // [T]
+  int* idx;                  // [T] token of a row
+  int* inv;                  // [T] row of a token, or -1
+  int* tgt;                  // [T] target of a row
+  int* counts;               // [0] all rows; [1 + c] rows of chunk c
+  float* lt;                 // [T] target's logit
+  float* ref;                // [T] reference logit of the row's sums
+  float* sum;                // [T] sum over the vocabulary but the target of exp(logit - ref)
+  float* alpha;              // [T] what the row's earlier sums were last rescaled by
+};
+// counted rows of all tokens, and of each chunk of `chunk` rows
+hipError_t launch_lm_rows(const LmRows& a, int chunk, int n_chunks, hipStream_t s);
+// lt, ref, sum = 0, tgt
+hipError_t launch_lm_targets(const LmRows& a, hipStream_t s);
+
+// One piece of the vocabulary for one chunk of rows: columns [v0, v0 + cols), rows [m0, m0 + rows_max)
+struct LmPiece {
+  int m0, rows_max, v0, cols;
+  int pitch;                 // of e, and of the fp32 logits: cols rounded up to 64
+  const int* count;          // rows of the chunk (device)
+  void* e;                   // [rows_max][pitch] exp(logit - ref) (bf16; fp32: first the logits); null: sums only
+  float2* part;              // bf16: [rows_max][lm_parts(cols)] {reference, sum} of a row's pieces
+  float* acc;                // [slices][rows_max][d] sum over the vocabulary of e W
+  int slices;
+  bool first;                // acc is written, not added to
+};
+int lm_parts(int cols);
+int lm_dx_slices(int rows_max, int d, int depth);
+hipError_t launch_lm_logits(const LmRows& a, const LmPiece& p, hipStream_t s);
+// the row's sums with this piece's; e in units of the row's reference after it
+hipError_t launch_lm_combine(const LmRows& a, const LmPiece& p, hipStream_t s);
+hipError_t launch_lm_dx(const LmRows& a, const LmPiece& p, const void* w_t, int ld_wt, hipStream_t s);
+
+struct LmFinish {
+  int m0, chunk, slices;     // rows [m0, m0 + chunk) are complete
+  bool last;                 // no chunk after this one: the loss, and the tokens that do not count
+  const float* acc;          // [slices][chunk][d]
+  float scale;
+  bool mean;
+  float *loss, *token_loss;  // token_loss may be null
+  void* dx;                  // null: none wanted
+  float *lse, *own;          // [T] of a row for dW: log sum of its logits, p - 1 of its target; null: none wanted
+};
+hipError_t launch_lm_finish(const LmRows& a, const LmFinish& f, hipStream_t s);
+
+// dW of the columns [v0, v0 + cols), all rows at once.  g [cols][pitch]: the loss's gradient over the logits, the
+// rows contiguous, zero behind the last; xT [d][pitch]: the counted rows of x, transposed, zero likewise.
+// bf16: launch_lm_g forms the logits anew and leaves the unit scale / N to launch_lm_dw; fp32: launch_lm_g_f32 from the
+// logits [T][ldl] of launch_lm_logits, unit included.
+hipError_t launch_lm_xT(const LmRows& a, void* xT, int pitch, hipStream_t s);
+hipError_t launch_lm_g(const LmRows& a, int v0, int cols, const float* lse, const float* own, void* g, int pitch,
+                       hipStream_t s);
+hipError_t launch_lm_g_f32(const LmRows& a, int v0, int cols, const float* lse, const float* own, const float* logits,
+                           int ldl, float scale, bool mean, float* g, int pitch, hipStream_t s);
+hipError_t launch_lm_dw(const LmRows& a, int v0, int cols, const void* g, const void* xT, int pitch, float scale, bool mean,
+                        void* dw, hipStream_t s);
+
 }  // namespace hero

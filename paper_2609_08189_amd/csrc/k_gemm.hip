@@ -58,6 +58,9 @@ struct BRows {
   const T* b1;
   int split;
   int ld;
+  // the large products: rows past the last one repeat it, and rows may be gathered
+  int last = INT_MAX;
+  const int* idx = nullptr;
   __device__ __forceinline__ const T* row(int n) const {
     return n < split ? b0 + static_cast<size_t>(n) * ld : b1 + static_cast<size_t>(n - split) * ld;
   }
@@ -556,6 +559,22 @@ struct TwoTerm : std::false_type {};
 template <class E>
 struct TwoTerm<E, std::void_t<decltype(E::kTwoTerm)>> : std::true_type {};
 
+// An epilogue with kColumns prepares what its columns combine with once a tile (Epi::Cols, for the eight
+// columns that a lane emits in every row block); skip(n0) leaves a tile of columns out.
+template <class E, class = void>
+struct ColumnsHook : std::false_type {
+  struct Cols {};
+};
+template <class E>
+struct ColumnsHook<E, std::void_t<decltype(E::kColumns)>> : std::true_type {
+  using Cols = typename E::Cols;
+};
+// An epilogue with kDeviceDepth knows K on the device: depth(), at most the host's
+template <class E, class = void>
+struct DeviceDepth : std::false_type {};
+template <class E>
+struct DeviceDepth<E, std::void_t<decltype(E::kDeviceDepth)>> : std::true_type {};
+
 template <int BM_, bool DUAL_>
 struct Phase {
   static constexpr int WN = 4, NW = 8, NT = 512;
@@ -591,6 +610,9 @@ __device__ __forceinline__ void phase_tile(const ARows<bf16_t>& A, const BRows<b
   const int grp = tile / (GROUP_M * n_tiles), rem = tile % (GROUP_M * n_tiles);
   const int gsz = min(GROUP_M, mt_act - grp * GROUP_M);
   const int mt = grp * GROUP_M + rem % gsz, nt = rem / gsz;
+  if constexpr (ColumnsHook<Epi>::value)
+    if (epi.skip(nt * C::BN)) return;
+  if constexpr (DeviceDepth<Epi>::value) K = epi.depth();
   const int m0 = mt * BM;
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) >> 6);
@@ -614,7 +636,8 @@ __device__ __forceinline__ void phase_tile(const ARows<bf16_t>& A, const BRows<b
     const int r = blk + rsub;
     const int ch = (lane & 7) ^ ((r >> 1) & 7);
     const bool second = C::DUAL ? blk >= 128 : nt * 256 + blk >= B.split;
-    const int row = C::DUAL ? nt * 128 + (r & 127) : nt * 256 + r - (second ? B.split : 0);
+    int row = min(C::DUAL ? nt * 128 + (r & 127) : nt * 256 + r - (second ? B.split : 0), B.last);
+    if (B.idx) row = B.idx[row];
     b_base[i] = reinterpret_cast<const unsigned char*>(second ? B.b1 : B.b0);
     b_off[i] = static_cast<uint32_t>(row) * static_cast<uint32_t>(B.ld * 2) + ch * 16;
   }
@@ -799,6 +822,8 @@ __device__ __forceinline__ void phase_tile(const ARows<bf16_t>& A, const BRows<b
         pre[a][p] = epi.prep(min(row_of(a, e / CPR), M - 1), col_of((e % CPR) * 8));
       }
     };
+    typename ColumnsHook<Epi>::Cols cols;
+    if constexpr (ColumnsHook<Epi>::value) cols = epi.cols(col_of((lane % CPR) * 8));   // CPR divides the wave
     // what the epilogue combines with (hbar rows) is fetched some fragments ahead of the staging
     constexpr int AHEAD = TwoTerm<Epi>::value ? 2 : 4;
 #pragma unroll
@@ -818,7 +843,11 @@ __device__ __forceinline__ void phase_tile(const ARows<bf16_t>& A, const BRows<b
         for (int p = 0; p < PP; ++p) {
           const int e = lane + kWave * p, i = e / CPR, c8 = (e % CPR) * 8;
           const int m = row_of(a, i);
-          if (m < M) epi.emit8(pre[a][p], m, col_of(c8), stg + i * OP + c8);
+          if constexpr (ColumnsHook<Epi>::value) {
+            if (m < M) epi.emit8(cols, m, col_of(c8), stg + i * OP + c8);
+          } else {
+            if (m < M) epi.emit8(pre[a][p], m, col_of(c8), stg + i * OP + c8);
+          }
         }
       }
     }
@@ -2959,6 +2988,232 @@ hipError_t launch_gemm_nt_f32(const void* A, int M, const void* B, int N, int K,
   ARows<bf16_t> a{static_cast<const bf16_t*>(A), nullptr, K};
   BRows<bf16_t> b{static_cast<const bf16_t*>(B), nullptr, INT_MAX, K};
   return run_tile<TileWide>(a, b, EpiStoreF32{C, ldc, 0}, nullptr, M, N, K, s);
+}
+
+// ---------------------------------------------------------------------------
+// Language-model loss (k_lm_loss.hip has the formulas): the products over one piece of the vocabulary.
+//   logits   l = x[idx] W^T                   -> e = exp(l - ref) in bf16, and its sums a row and wave
+//   dx       acc (+)= e W                     B = W^T [d][pitch of the vocabulary]
+//   dW       g = c (p - [target])^T = W x^T   -> bf16, the tokens contiguous; dW = g x, B = x^T
+// ---------------------------------------------------------------------------
+namespace {
+
+// Where a logit may stand above its row's reference before the piece takes one of its own: e stays far
+// from the end of the range (e^60 summed over any vocabulary, times any weight, is below 2^120).
+constexpr float kLmAbove = 60.0f;
+
+// e[m][n] = exp(l - ref_m) for every column but the target's, whose share is kept apart (1 - p of a sure
+// token would cancel in it).  ref is the target's logit, or what the row's earlier pieces raised it to, so
+// no pass for a maximum is needed: e is a floating number whatever its size.  Where a logit is more than
+// kLmAbove over it, the wave's 64 columns of that row take their own maximum as reference, and the pass
+// over the partial sums brings them together.  The 64 columns of a row sit in eight neighbouring lanes.
+template <bool STORE>
+struct EpiLmExp {
+  const float* ref;
+  const int* tgt;
+  int v0, cols, pitch;
+  bf16_t* e;
+  float2* part;
+  int parts;
+  struct Pre {
+    float ref;
+    int tgt;
+  };
+  __device__ __forceinline__ Pre prep(int m, int) const { return {ref[m], tgt[m] - v0}; }
+  __device__ __forceinline__ void emit8(const Pre& p, int m, int n, const float* v) const {
+    float r = p.ref, x[8];
+    bool above = false;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      x[k] = v[k];
+      above |= x[k] - r > kLmAbove && n + k < cols;
+    }
+    if (__any(above)) {
+      float mx = r;
+#pragma unroll
+      for (int k = 0; k < 8; ++k)
+        if (n + k < cols) mx = fmaxf(mx, x[k]);
+      mx = fmaxf(mx, __shfl_xor(mx, 1, 8));
+      mx = fmaxf(mx, __shfl_xor(mx, 2, 8));
+      mx = fmaxf(mx, __shfl_xor(mx, 4, 8));
+      if (mx - r > kLmAbove) r = mx;
+    }
+    float s = 0.f;
+    u32x4 w;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      x[k] = n + k < cols && n + k != p.tgt ? __expf(x[k] - r) : 0.f;
+      s += x[k];
+    }
+    if constexpr (STORE) {
+      if (n < pitch) st8(e + static_cast<size_t>(m) * pitch + n, x);
+    }
+    s = group_sum<8>(s);
+    if ((threadIdx.x & 7) == 0) part[static_cast<size_t>(m) * parts + (n >> 8) * 4 + ((n & 127) >> 5)] = {r, s};
+  }
+};
+
+// acc[m][n] = alpha_m acc[m][n] + the piece's product
+struct EpiLmAcc {
+  float* out;
+  int ld;
+  size_t split_stride;
+  const float* alpha;
+  struct Pre {
+    f32x4 o[2];
+    float a;
+  };
+  __device__ __forceinline__ float* at(int m, int n) const {
+    return out + blockIdx.y * split_stride + static_cast<size_t>(m) * ld + n;
+  }
+  __device__ __forceinline__ Pre prep(int m, int n) const {
+    const float* o = at(m, n);
+    return {{*reinterpret_cast<const f32x4*>(o), *reinterpret_cast<const f32x4*>(o + 4)}, alpha[m]};
+  }
+  __device__ __forceinline__ void emit8(const Pre& p, int m, int n, const float* v) const {
+    float* o = at(m, n);
+    *reinterpret_cast<f32x4*>(o) = p.a * p.o[0] + *reinterpret_cast<const f32x4*>(v);
+    *reinterpret_cast<f32x4*>(o + 4) = p.a * p.o[1] + *reinterpret_cast<const f32x4*>(v + 4);
+  }
+  // fp32 products: no K slices
+  __device__ __forceinline__ void store(int m, int n, float v) const {
+    float* o = out + static_cast<size_t>(m) * ld + n;
+    *o = fmaf(alpha[m], *o, v);
+  }
+};
+
+// columns of the tokens that a product over them as K runs through: at least two k-tiles
+__device__ __forceinline__ int lm_depth(const int* count) { return max(2 * BK, (*count + BK - 1) / BK * BK); }
+
+// g[v][t] = p_tv - [v = target of t] for the counted rows t, zero behind them (the unit, scale / N, is
+// dW's epilogue's); columns: the tokens' log sums and targets
+struct EpiLmG {
+  static constexpr bool kColumns = true;
+  const float *lse, *own;    // [rows] log sum of a row, p - 1 of its target
+  const int *tgt, *count;
+  int v0, pitch;
+  bf16_t* g;
+  struct Cols {
+    float lse[8];
+    int tgt[8];
+  };
+  struct Pre {};
+  __device__ __forceinline__ Pre prep(int, int) const { return {}; }
+  __device__ __forceinline__ bool skip(int n0) const { return n0 >= lm_depth(count); }
+  __device__ __forceinline__ Cols cols(int n) const {
+    Cols c;
+    const int N = *count;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const bool in = n + k < N;
+      c.lse[k] = in ? lse[n + k] : 0.f;
+      c.tgt[k] = in ? tgt[n + k] - v0 : INT_MIN;
+    }
+    return c;
+  }
+  __device__ __forceinline__ void emit8(const Cols& c, int m, int n, const float* v) const {
+    if (n >= pitch) return;
+    float x[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      x[k] = c.tgt[k] == INT_MIN ? 0.f : __expf(v[k] - c.lse[k]);
+      if (c.tgt[k] == m) x[k] = own[n + k];
+    }
+    st8(g + static_cast<size_t>(m) * pitch + n, x);
+  }
+};
+
+struct EpiLmDw {   // dw[m][n] = unit acc, the tokens as K
+  static constexpr bool kDeviceDepth = true;
+  bf16_t* out;
+  int ld;
+  const int* count;
+  float scale;
+  bool mean;
+  struct Pre {
+    float c;
+  };
+  __device__ __forceinline__ int depth() const { return lm_depth(count); }
+  __device__ __forceinline__ Pre prep(int, int) const { return {mean ? scale / static_cast<float>(max(*count, 1)) : scale}; }
+  __device__ __forceinline__ void emit8(const Pre& p, int m, int n, const float* v) const {
+    float x[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) x[k] = p.c * v[k];
+    st8(out + static_cast<size_t>(m) * ld + n, x);
+  }
+};
+
+int lm_tiles(int n) { return (n + 255) / 256; }
+
+}  // namespace
+
+int lm_parts(int cols) { return 4 * lm_tiles(cols); }
+
+// K slices of the dx product: 128-row tiles that leave CUs idle share them, a slice of at least four k-tiles
+int lm_dx_slices(int rows_max, int d, int depth) {
+  const int tiles = (rows_max + 127) / 128 * (d / 256);
+  return std::max(1, std::min({kCUs / std::max(tiles, 1), depth / (4 * BK), 64}));
+}
+
+hipError_t launch_lm_logits(const LmRows& a, const LmPiece& p, hipStream_t s) {
+  const size_t w0 = static_cast<size_t>(p.v0) * a.d;
+  if (a.dtype != 1) {
+    ARows<float> A{static_cast<const float*>(a.x), a.idx + p.m0, a.d};
+    BRows<float> B{static_cast<const float*>(a.w) + w0, nullptr, INT_MAX, a.d};
+    return run_f32<false>(A, B, EpiStoreF32{static_cast<float*>(p.e), p.pitch, 0}, p.count, p.rows_max, p.cols, a.d, s);
+  }
+  ARows<bf16_t> A{static_cast<const bf16_t*>(a.x), a.idx + p.m0, a.d};
+  BRows<bf16_t> B{static_cast<const bf16_t*>(a.w) + w0, nullptr, INT_MAX, a.d, p.cols - 1};
+  const float* ref = a.ref + p.m0;
+  const int *tgt = a.tgt + p.m0, parts = lm_parts(p.cols), n = lm_tiles(p.cols) * 256;
+  bf16_t* e = static_cast<bf16_t*>(p.e);
+  if (e)
+    return run_phase<false>(A, B, EpiLmExp<true>{ref, tgt, p.v0, p.cols, p.pitch, e, p.part, parts}, p.count, p.rows_max,
+                            n, a.d, s, false);
+  return run_phase<false>(A, B, EpiLmExp<false>{ref, tgt, p.v0, p.cols, p.pitch, e, p.part, parts}, p.count, p.rows_max,
+                          n, a.d, s, false);
+}
+
+hipError_t launch_lm_dx(const LmRows& a, const LmPiece& p, const void* w_t, int ld_wt, hipStream_t s) {
+  const float* alpha = a.alpha + p.m0;
+  if (a.dtype != 1) {
+    ARows<float> A{static_cast<const float*>(p.e), nullptr, p.pitch};
+    BRows<float> B{static_cast<const float*>(w_t) + p.v0, nullptr, INT_MAX, ld_wt};
+    if (p.first) return run_f32<false>(A, B, EpiStoreF32{p.acc, a.d, 0}, p.count, p.rows_max, a.d, p.pitch, s);
+    return run_f32<false>(A, B, EpiLmAcc{p.acc, a.d, 0, alpha}, p.count, p.rows_max, a.d, p.pitch, s);
+  }
+  ARows<bf16_t> A{static_cast<const bf16_t*>(p.e), nullptr, p.pitch};
+  BRows<bf16_t> B{static_cast<const bf16_t*>(w_t) + p.v0, nullptr, INT_MAX, ld_wt};
+  const size_t stride = static_cast<size_t>(p.rows_max) * a.d;
+  const EpiStoreF32 st{p.acc, a.d, stride};
+  const EpiLmAcc add{p.acc, a.d, stride, alpha};
+  if (p.slices > 1)
+    return p.first ? run_phase_split(A, B, st, p.count, p.rows_max, a.d, p.pitch, p.slices, s)
+                   : run_phase_split(A, B, add, p.count, p.rows_max, a.d, p.pitch, p.slices, s);
+  return p.first ? run_phase<false>(A, B, st, p.count, p.rows_max, a.d, p.pitch, s, false)
+                 : run_phase<false>(A, B, add, p.count, p.rows_max, a.d, p.pitch, s, false);
+}
+
+hipError_t launch_lm_g(const LmRows& a, int v0, int cols, const float* lse, const float* own, void* g, int pitch,
+                       hipStream_t s) {
+  ARows<bf16_t> A{static_cast<const bf16_t*>(a.w) + static_cast<size_t>(v0) * a.d, nullptr, a.d};
+  BRows<bf16_t> B{static_cast<const bf16_t*>(a.x), nullptr, INT_MAX, a.d, a.T - 1, a.idx};
+  const EpiLmG epi{lse, own, a.tgt, a.counts, v0, pitch, static_cast<bf16_t*>(g)};
+  return run_phase<false>(A, B, epi, nullptr, cols, lm_tiles(pitch) * 256, a.d, s);
+}
+
+hipError_t launch_lm_dw(const LmRows& a, int v0, int cols, const void* g, const void* xT, int pitch, float scale, bool mean,
+                        void* dw, hipStream_t s) {
+  const size_t at = static_cast<size_t>(v0) * a.d;
+  if (a.dtype != 1) {   // g has the unit already
+    ARows<float> A{static_cast<const float*>(g), nullptr, pitch};
+    BRows<float> B{static_cast<const float*>(xT), nullptr, INT_MAX, pitch};
+    return run_f32<false>(A, B, EpiStore<float>{static_cast<float*>(dw) + at, a.d}, nullptr, cols, a.d, pitch, s);
+  }
+  ARows<bf16_t> A{static_cast<const bf16_t*>(g), nullptr, pitch};
+  BRows<bf16_t> B{static_cast<const bf16_t*>(xT), nullptr, INT_MAX, pitch};
+  const EpiLmDw epi{static_cast<bf16_t*>(dw) + at, a.d, a.counts, scale, mean};
+  return run_phase<false>(A, B, epi, nullptr, cols, a.d, pitch, s);
 }
 
 }  // namespace hero

@@ -34,6 +34,9 @@ HERO_F32 = 0
 HERO_BF16 = 1
 HERO_MODE_THRESHOLD = 0
 HERO_MODE_BUDGET = 1
+HERO_LOSS_SUM = 0
+HERO_LOSS_MEAN = 1
+HERO_GRAD_MAX_TENSORS = 4096
 HERO_ABL_NO_POS_STATE = 1
 HERO_ABL_NO_AUX_STATE = 2
 HERO_ABL_NO_MEMREAD = 4
@@ -44,7 +47,9 @@ KERNELS = ("rowstats", "router_gemm", "router_pre", "router_mem", "router_post",
            "attn_norm", "attn_qkv", "attn_core", "attn_out",
            "bwd_norm", "bwd_ffn_e", "bwd_ffn_gate_up", "bwd_ffn_du", "bwd_adapter", "bwd_adapter_wgrad",
            "bwd_rows", "skip_penalty",
-           "router_bwd_gemm", "router_bwd_token", "router_bwd_products", "router_bwd_rows")
+           "router_bwd_gemm", "router_bwd_token", "router_bwd_products", "router_bwd_rows",
+           "final_norm", "final_norm_bwd", "lm_rows", "lm_logits", "lm_combine", "lm_dx", "lm_finish", "lm_dw",
+           "grad_norm", "grad_clip")
 HERO_K = {name: i for i, name in enumerate(KERNELS)}
 
 _vp = ctypes.c_void_p
@@ -116,6 +121,18 @@ class hero_block_grads(ctypes.Structure):
 class hero_layer_stats(ctypes.Structure):
     _fields_ = [("mask", _vp), ("idx_ffn", _vp), ("idx_ad", _vp), ("counts", _vp),
                 ("logit", _vp), ("gate", _vp), ("lambda_", _vp)]
+
+
+class hero_lm_head(ctypes.Structure):
+    _fields_ = [("w", _vp), ("w_t", _vp)]
+
+
+class hero_lm_loss_out(ctypes.Structure):
+    _fields_ = [("loss", _vp), ("token_loss", _vp), ("dx", _vp), ("dw", _vp)]
+
+
+class hero_grad_tensor(ctypes.Structure):
+    _fields_ = [("grad", _vp), ("out", _vp), ("count", ctypes.c_size_t), ("dtype", ctypes.c_int)]
 
 
 _lib = None
@@ -200,6 +217,27 @@ def lib() -> ctypes.CDLL:
         L.hero_router_backward.argtypes = [P(hero_dims), ctypes.c_int, ctypes.c_int, _vp, _vp, _vp, P(hero_state),
                                            P(hero_router_weights), ctypes.c_float, _vp, P(hero_router_carry), _vp,
                                            _vp, _vp, P(hero_router_grads), _vp, _vp, ctypes.c_size_t, _vp]
+        L.hero_final_norm.restype = ctypes.c_int
+        L.hero_final_norm.argtypes = [P(hero_dims), ctypes.c_int, _vp, _vp, _vp, _vp]
+        L.hero_final_norm_backward_workspace_size.restype = ctypes.c_int
+        L.hero_final_norm_backward_workspace_size.argtypes = [P(hero_dims), ctypes.c_int, P(ctypes.c_size_t)]
+        L.hero_final_norm_backward.restype = ctypes.c_int
+        L.hero_final_norm_backward.argtypes = [P(hero_dims), ctypes.c_int, _vp, _vp, _vp, _vp, _vp, _vp,
+                                               ctypes.c_size_t, _vp]
+        L.hero_lm_head_weights_make.restype = ctypes.c_int
+        L.hero_lm_head_weights_make.argtypes = [P(hero_dims), ctypes.c_int, _vp, _vp, _vp]
+        L.hero_lm_loss_workspace_size.restype = ctypes.c_int
+        L.hero_lm_loss_workspace_size.argtypes = [P(hero_dims), ctypes.c_int, ctypes.c_int, ctypes.c_int, ctypes.c_int,
+                                                  P(ctypes.c_size_t)]
+        L.hero_lm_loss.restype = ctypes.c_int
+        L.hero_lm_loss.argtypes = [P(hero_dims), ctypes.c_int, ctypes.c_int, _vp, P(hero_lm_head), _vp, ctypes.c_int,
+                                   ctypes.c_float, P(hero_lm_loss_out), _vp, ctypes.c_size_t, _vp]
+        L.hero_grad_norm_workspace_size.restype = ctypes.c_int
+        L.hero_grad_norm_workspace_size.argtypes = [ctypes.c_int, P(hero_grad_tensor), P(ctypes.c_size_t)]
+        L.hero_grad_norm.restype = ctypes.c_int
+        L.hero_grad_norm.argtypes = [ctypes.c_int, P(hero_grad_tensor), _vp, _vp, ctypes.c_size_t, _vp]
+        L.hero_grad_clip.restype = ctypes.c_int
+        L.hero_grad_clip.argtypes = [ctypes.c_int, P(hero_grad_tensor), ctypes.c_float, _vp, _vp, ctypes.c_size_t, _vp]
         L.hero_peak_mfma.restype = ctypes.c_int
         L.hero_peak_mfma.argtypes = [ctypes.c_int, ctypes.c_int, ctypes.c_int, _vp, _vp, P(ctypes.c_double)]
         L.hero_peak_read.restype = ctypes.c_int
@@ -433,3 +471,63 @@ def hero_router_backward(dims: hero_dims, j: int, T: int, hbar, hbar_prev1, hbar
                                       _byref(state_in), _byref(router), float(eta), ptr(dlogit), _byref(carry),
                                       ptr(dhbar), ptr(dhbar_prev1), ptr(dhbar_prev2), _byref(grads), ptr(deta),
                                       ptr(workspace), workspace_bytes, stream)
+
+
+def hero_final_norm(dims: hero_dims, T: int, h, norm_w, x, stream=None) -> int:
+    """x = RMSNorm(h) * norm_w; returns the hero_status code."""
+    return lib().hero_final_norm(ctypes.byref(dims), T, ptr(h), ptr(norm_w), ptr(x), stream)
+
+
+def hero_final_norm_backward_workspace_size(dims: hero_dims, T: int) -> int:
+    out = ctypes.c_size_t(0)
+    check(lib().hero_final_norm_backward_workspace_size(ctypes.byref(dims), T, ctypes.byref(out)),
+          "hero_final_norm_backward_workspace_size")
+    return out.value
+
+
+def hero_final_norm_backward(dims: hero_dims, T: int, h, dx, norm_w, dh, dnorm_w, workspace, workspace_bytes: int,
+                             stream=None) -> int:
+    """dL/dh and (dnorm_w not None) the gain's gradient of the final norm; returns the hero_status code."""
+    return lib().hero_final_norm_backward(ctypes.byref(dims), T, ptr(h), ptr(dx), ptr(norm_w), ptr(dh), ptr(dnorm_w),
+                                          ptr(workspace), int(workspace_bytes), stream)
+
+
+def hero_lm_head_weights_make(dims: hero_dims, vocab: int, w, w_t, stream=None) -> int:
+    """Fill the head's transposed copy w_t [d][vocab rounded up to 64]."""
+    return lib().hero_lm_head_weights_make(ctypes.byref(dims), vocab, ptr(w), ptr(w_t), stream)
+
+
+def hero_lm_loss_workspace_size(dims: hero_dims, vocab: int, T: int, with_dx: bool, with_dw: bool) -> int:
+    out = ctypes.c_size_t(0)
+    check(lib().hero_lm_loss_workspace_size(ctypes.byref(dims), vocab, T, int(bool(with_dx)), int(bool(with_dw)),
+                                            ctypes.byref(out)), "hero_lm_loss_workspace_size")
+    return out.value
+
+
+def hero_lm_loss(dims: hero_dims, vocab: int, T: int, x, head: hero_lm_head, targets, reduction: int, scale: float,
+                 out: hero_lm_loss_out, workspace, workspace_bytes: int, stream=None) -> int:
+    """Enqueue the language-model loss and the gradients that out names; returns the hero_status code."""
+    return lib().hero_lm_loss(ctypes.byref(dims), vocab, T, ptr(x), _byref(head), ptr(targets), reduction, float(scale),
+                              _byref(out), ptr(workspace), int(workspace_bytes), stream)
+
+
+def hero_grad_tensors(items):
+    """A host list of (grad, out or None, count, dtype code) as the array that the gradient calls take."""
+    return (hero_grad_tensor * len(items))(*[hero_grad_tensor(ptr(g), ptr(o), n, dt) for g, o, n, dt in items])
+
+
+def hero_grad_norm_workspace_size(tensors) -> int:
+    out = ctypes.c_size_t(0)
+    check(lib().hero_grad_norm_workspace_size(len(tensors), tensors, ctypes.byref(out)), "hero_grad_norm_workspace_size")
+    return out.value
+
+
+def hero_grad_norm(tensors, norm, workspace, workspace_bytes: int, stream=None) -> int:
+    """norm[0] = global L2 norm of hero_grad_tensors(...); returns the hero_status code."""
+    return lib().hero_grad_norm(len(tensors), tensors, ptr(norm), ptr(workspace), int(workspace_bytes), stream)
+
+
+def hero_grad_clip(tensors, max_norm: float, norm, workspace, workspace_bytes: int, stream=None) -> int:
+    """The norm, and every tensor scaled by min(1, max_norm / norm) into its out; returns the hero_status code."""
+    return lib().hero_grad_clip(len(tensors), tensors, float(max_norm), ptr(norm), ptr(workspace), int(workspace_bytes),
+                                stream)

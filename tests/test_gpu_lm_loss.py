@@ -1,0 +1,259 @@
+"""hero_lm_loss against the oracle in 64 bits, element by element, within bounds derived from the roundings on the way
+(train_ends.loss_bounds)."""
+import numpy as np
+import pytest
+
+from oracle import hero_oracle as O
+
+pytestmark = pytest.mark.gpu
+
+
+def _inputs(T, d, V, dtype, seed, keep=0.8, size=1.0, sure=8.0):
+    import torch
+    from tests import train_ends as E
+    rng = np.random.default_rng(seed)
+    w = torch.from_numpy(rng.standard_normal((V, d)).astype(np.float32) * (1.5 / d ** 0.5)).to(E.DEV).to(E.TORCH[dtype])
+    y = rng.integers(0, V, T)
+    x = rng.standard_normal((T, d)).astype(np.float32)
+    x += (sure * rng.random((T, 1)) / 1.5).astype(np.float32) * w.float().cpu().numpy()[y]
+    y[rng.random(T) >= keep] = -1
+    return torch.from_numpy(x * np.float32(size)).to(E.DEV).to(E.TORCH[dtype]), w, y
+
+
+def _check(c, y):
+    from tests import train_ends as E
+    x, w = E.f64(c.x), E.f64(c.w)
+    worst = E.check_loss(c, O.lm_loss(x, w, y, c.scale, c.mean), E.loss_bounds(x, w, y, c.scale, c.mean, c.dtype))
+    print("  share of the bounds:", {k: f"{v:.2f}" for k, v in worst.items()}, flush=True)
+    for k in ("token_loss", "dx"):
+        if k in c.out:
+            lost = (y < 0) | (y >= c.V)
+            assert not E.f64(c.out[k].t)[lost].any(), f"{k} of a token that does not count"
+
+
+SIZES = [(1, 256, 65), (1, 512, 2003), (2, 256, 127), (3, 256, 128), (17, 512, 256), (63, 256, 257), (64, 768, 320),
+         (65, 256, 1000), (129, 512, 4001), (257, 256, 2003), (300, 1024, 511), (600, 256, 3001), (1025, 256, 1537)]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("T,d,V", SIZES)
+def test_loss_and_gradients(T, d, V, dtype):
+    from tests import train_ends as E
+    print(f"case lm_loss T={T} d={d} V={V} {dtype}", flush=True)
+    x, w, y = _inputs(T, d, V, dtype, T + V, keep=1.0 if T < 4 else 0.8)
+    _check(E.Loss(x, w, y, mean=T % 2 == 1, scale=1.0 if T % 2 else 0.37).run(), y)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("dx,dw", [(False, False), (True, False), (False, True)])
+def test_outputs_are_optional(dx, dw, dtype):
+    import torch
+    from tests import train_ends as E
+    print(f"case lm_loss outputs dx={dx} dw={dw} {dtype}", flush=True)
+    x, w, y = _inputs(150, 512, 1333, dtype, 5)
+    c, full = E.Loss(x, w, y, dx=dx, dw=dw).run(), E.Loss(x, w, y).run()
+    _check(c, y)
+    for k in c.out:
+        assert torch.equal(c.out[k].t, full.out[k].t), k
+
+
+@pytest.mark.parametrize("T,V,dtype", [(8192 + 9, 16384 + 300, "bf16"), (8192 + 9, 8192 + 200, "f32"), (8192, 32768 + 77, "bf16")])
+def test_chunks_of_rows_and_pieces_of_the_vocabulary(T, V, dtype):
+    from tests import train_ends as E
+    print(f"case lm_loss pieces T={T} V={V} {dtype}", flush=True)
+    x, w, y = _inputs(T, 256, V, dtype, 1, keep=0.97)
+    _check(E.Loss(x, w, y, dw=dtype == "bf16").run(), y)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("T,size", [(5, 30.0), (200, 30.0), (200, 120.0)])
+def test_logits_far_above_the_target(T, size, dtype):
+    """References move: differences of several hundred between a row's logits."""
+    from tests import train_ends as E
+    print(f"case lm_loss far T={T} size={size} {dtype}", flush=True)
+    x, w, y = _inputs(T, 256, 1700, dtype, 11, keep=0.9, size=size, sure=2.0)
+    _check(E.Loss(x, w, y, mean=False).run(), y)
+
+
+def test_reference_moves_between_pieces():
+    """The target in the first piece, a logit 200 above it in the last, another 150 above it before."""
+    import torch
+    from tests import train_ends as E
+    T, d, V = 8192, 256, 40000
+    print("case lm_loss far, by pieces", flush=True)
+    g = torch.Generator().manual_seed(3)
+    w = torch.randn(V, d, generator=g) * 0.02
+    x = torch.randn(T, d, generator=g)
+    w[20000] = x[5] / x[5].norm() * 9.5
+    w[39999] = x[5] / x[5].norm() * 13.0
+    w[30000] = -x[7] / x[7].norm() * 14.0
+    x, w = x.to(E.DEV).bfloat16(), w.to(E.DEV).bfloat16()
+    y = np.full(T, -1)
+    y[[0, 5, 7, 4000, 8191]] = [9, 100, 30000, 39999, 20000]
+    _check(E.Loss(x, w, y, dw=False).run(), y)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_sure_tokens_keep_the_digits_of_their_loss(dtype):
+    from tests import train_ends as E
+    print(f"case lm_loss sure {dtype}", flush=True)
+    x, w, y = _inputs(64, 256, 700, dtype, 4, keep=1.0, sure=30.0)
+    c = E.Loss(x, w, y).run()
+    _check(c, y)
+    ref = O.lm_loss(E.f64(x), E.f64(w), y).token_loss
+    small = ref < 1e-3
+    assert small.sum() > 10
+    # a relative error of the loss: that of exp at arguments of some tens, and the logits' (256 additions of fp32)
+    assert np.all(np.abs(E.f64(c.out["token_loss"].t)[small] / ref[small] - 1) < 256 * 2.0 ** -24 * 60)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_tokens_that_do_not_count(dtype):
+    """None counts; targets at both ends of int32; rows of NaN and infinity without a target."""
+    import torch
+    from tests import train_ends as E
+    print(f"case lm_loss ignored {dtype}", flush=True)
+    T, V = 90, 400
+    x, w, y = _inputs(T, 256, V, dtype, 9, keep=1.0)
+    y[::3], y[1::9], y[5] = -100, V, 2 ** 31 - 1
+    y[8] = -2 ** 31
+    x[::3] = float("nan")
+    x[1::9] = float("inf")
+    c = E.Loss(x, w, y).run()
+    got = c.results()
+    clean = x.clone()
+    clean[torch.from_numpy((y < 0) | (y >= V)).to(E.DEV)] = 0
+    ref = O.lm_loss(E.f64(clean), E.f64(w), y)
+    E.check_loss(c, ref, E.loss_bounds(E.f64(clean), E.f64(w), y, 1.0, True, dtype), got)
+    assert not got["dx"][(y < 0) | (y >= V)].any()
+    for mean in (True, False):
+        none = E.Loss(x, w, np.full(T, -1), mean=mean).run().results()
+        assert all(not v.any() for v in none.values())
+
+
+def test_one_counted_token_anywhere():
+    from tests import train_ends as E
+    x, w, _ = _inputs(2500, 256, 600, "bf16", 2)
+    for t in (0, 1, 1023, 1024, 2499):
+        print(f"case lm_loss one counted token {t}", flush=True)
+        y = np.full(2500, -1)
+        y[t] = 599
+        _check(E.Loss(x, w, y).run(), y)
+
+
+def test_nan_in_one_token_stays_there():
+    import torch
+    from tests import train_ends as E
+    print("case lm_loss nan", flush=True)
+    x, w, y = _inputs(130, 256, 500, "bf16", 6, keep=1.0)
+    x[70, 3] = float("nan")
+    x[71] = 3e38           # its logits overflow
+    c = E.Loss(x, w, y, mean=False, dw=False).run()
+    got = c.results()
+    assert np.isnan(got["loss"]).all() and np.isnan(got["token_loss"][70:72]).all() and np.isnan(got["dx"][70:72]).all()
+    rest = np.r_[0:70, 72:130]
+    assert np.isfinite(got["token_loss"][rest]).all() and np.isfinite(got["dx"][rest]).all()
+    alone = E.Loss(x[:70], w, y[:70], mean=False, dw=False).run()
+    torch.cuda.synchronize()
+    assert torch.equal(alone.out["token_loss"].t, c.out["token_loss"].t[:70])
+
+
+def test_head_copy_is_the_transpose_with_zeros():
+    import torch
+    from tests import train_ends as E
+    for dtype in ("bf16", "f32"):
+        for d, V in [(256, 65), (512, 128), (256, 1001), (1280, 70)]:
+            print(f"case head copy d={d} V={V} {dtype}", flush=True)
+            x, w, y = _inputs(1, d, V, dtype, V)
+            c = E.Loss(x, w, y, dw=False)
+            torch.cuda.synchronize()
+            assert c.w_t.whole() and torch.equal(c.w_t.t[:, :V], w.t()) and not c.w_t.t[:, V:].any()
+
+
+def test_head_beyond_32_bit_offsets():
+    """300000 rows of 8192: 4.9 GB, scored in pieces."""
+    import torch
+    from tests import train_ends as E
+    print("case lm_loss 300000 x 8192", flush=True)
+    V, d, T = 300000, 8192, 3
+    g = torch.Generator(device=E.DEV).manual_seed(1)
+    w = torch.empty(V, d, dtype=torch.bfloat16, device=E.DEV)
+    for i in range(0, V, 50000):
+        w[i:i + 50000] = torch.randn(50000, d, generator=g, device=E.DEV) * 0.02
+    x = torch.randn(T, d, generator=g, device=E.DEV).bfloat16()
+    y = np.array([5, 299999, 150000])
+    c = E.Loss(x, w, y, dx=False, dw=False).run()
+    got = c.results()
+    logits = torch.cat([x.double() @ w[i:i + 50000].double().t() for i in range(0, V, 50000)], 1)
+    ref = torch.logsumexp(logits, 1) - logits[torch.arange(T), torch.as_tensor(y)]
+    # the logits' relative error: 8192 additions of |x W| about 0.8 0.016 each, twice; far above the rest
+    assert np.all(np.abs(got["token_loss"] - ref.cpu().numpy()) < 2 * 8192 * 2.0 ** -24 * 8192 * 0.8 * 0.016)
+    assert np.all(np.abs(got["token_loss"] - ref.cpu().numpy()) < 1e-4)
+    del w, logits
+    torch.cuda.empty_cache()
+
+
+def test_calls_repeat_bit_for_bit_and_leave_inputs_alone():
+    import torch
+    from tests import train_ends as E
+    print("case lm_loss repeat", flush=True)
+    x, w, y = _inputs(700, 512, 5000, "bf16", 8)
+    c = E.Loss(x, w, y).run()
+    torch.cuda.synchronize()
+    first, x0, w0 = {k: v.t.clone() for k, v in c.out.items()}, x.clone(), w.clone()
+    for v in c.out.values():
+        v.poison()
+    c.ws.poison()
+    c.run()
+    torch.cuda.synchronize()
+    assert all(torch.equal(first[k], v.t) for k, v in c.out.items())
+    assert torch.equal(x, x0) and torch.equal(w, w0)
+
+
+def test_two_calls_on_two_streams():
+    import torch
+    from tests import train_ends as E
+    print("case lm_loss two streams", flush=True)
+    a, b = _inputs(500, 512, 3000, "bf16", 21), _inputs(333, 512, 2500, "bf16", 22)
+    ca, cb = E.Loss(*a), E.Loss(*b)
+    sa, sb = torch.cuda.Stream(), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for _ in range(3):
+        with torch.cuda.stream(sa):
+            ca.run()
+        with torch.cuda.stream(sb):
+            cb.run()
+    _check(ca, a[2])
+    _check(cb, b[2])
+
+
+@pytest.mark.parametrize("T,dtype", [(5, "bf16"), (300, "bf16"), (70, "f32")])
+def test_graph_replays_with_new_inputs(T, dtype):
+    """Targets, and with them the number of rows, change between the replays; eager work runs in between."""
+    import torch
+    from tests import train_ends as E
+    print(f"case lm_loss graph T={T} {dtype}", flush=True)
+    x, w, y = _inputs(T, 512, 2003, dtype, 13, keep=1.0)
+    c = E.Loss(x, w, y).run()
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        c.run()
+    torch.cuda.synchronize()
+    junk = torch.randn(1 << 20, device=E.DEV)
+    rng = np.random.default_rng(0)
+    for keep in (1.0, 0.4, 0.0, 0.9):
+        x2, _, _ = _inputs(T, 512, 2003, dtype, 100 + int(10 * keep), keep=1.0)
+        y2 = np.where(rng.random(T) < keep, rng.integers(0, 2003, T), -1)
+        c.x.copy_(x2)
+        c.y.copy_(torch.as_tensor(y2, dtype=torch.int32))
+        eager = E.Loss(x2, w, y2).run()
+        for v in c.out.values():
+            v.poison()
+        junk.mul_(1.0001)
+        torch.cuda.synchronize()
+        g.replay()
+        torch.cuda.synchronize()
+        for k, v in c.out.items():
+            assert v.whole() and torch.equal(v.t, eager.out[k].t), f"keep {keep}: {k}"
+    del g
