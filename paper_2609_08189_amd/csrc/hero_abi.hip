@@ -1705,15 +1705,24 @@ bool any_overlap(const Region (&written)[W], const Region (&read)[R]) {
 constexpr int kLmChunk = 8192;               // rows of one chunk
 constexpr size_t kLmPieceBytes = 256u << 20; // of e (or of dW's g) for one chunk and piece: the last-level cache's size
 constexpr int kLmVocabMax = 65535 * 64;      // grid limit of the head's transpose
-constexpr int kLmVocabMin = 65;              // bf16: the products take K in at least two k-tiles
+constexpr int kLmVocabMin = 65;              // matrix cores: the products take K in at least two k-tiles
 constexpr int kLmHeadRows = 1 << 17;         // head rows of a product, which addresses them with 32 bits
 
+// fp32 models: from so many tokens on the products of three-term operands are faster than those on the fp32 matrix
+// cores, which read operands without LDS: the head's terms cost a pass over it (4 bytes read, 6 written an
+// element), a row 2 d operations at 75 against 230 TFLOP/s.
+constexpr int kLmSplitRows = 128;
+
 struct LmLayout {
+  int mode;
   int chunk, n_chunks;       // rows of a chunk, chunks of T rows
   int cols, pieces, pitch;   // columns of a piece (the last takes the rest), widest piece's pitch
-  int slices;                // K slices of the dx products
+  int slices, ldl;           // K slices of the logits, 0: none kept; their pitch
+  bool single;               // one piece and one chunk: dW is formed from e
+  bool keep_e;
+  int acc_rows, dx_depth, f32_slices;
   int g_cols, g_pitch, g_ldl;
-  size_t idx, inv, tgt, counts, lt, ref, sum, alpha, e, part, acc, lse, own, g, xT, logits, total;
+  size_t idx, inv, tgt, counts, plan, done, lt, ref, sum, alpha, nll, lse, own, e, part, acc, g, xT, logits, xs, ws, wts, total;
 };
 
 int lm_piece_cols(const LmLayout& L, int vocab, int k) { return k == L.pieces - 1 ? vocab - k * L.cols : L.cols; }
@@ -1726,42 +1735,69 @@ LmLayout lm_layout_of(const hero_dims& d, int vocab, int T, bool dx, bool dw) {
     off = align_up(off + bytes);
     return o;
   };
-  const size_t t = static_cast<size_t>(T), es = esize(d.dtype);
-  const bool mfma = d.dtype == HERO_BF16;
-  auto up64 = [](int n) { return (n + 63) / 64 * 64; };
-  // whole tiles of 256 columns whose rows fit the piece; the loss alone keeps no e in bf16, only the sums
+  const size_t t = static_cast<size_t>(T), w = static_cast<size_t>(d.d);
+  auto up = [](int n, int k) { return (n + k - 1) / k * k; };
+  const bool split = d.dtype != HERO_BF16 && T >= kLmSplitRows && d.d % 256 == 0 && vocab >= kLmVocabMin &&
+                     (t + 128) * w * 2 < static_cast<size_t>(kGemmSpan) && T <= 1 << 19;
+  L.mode = d.dtype == HERO_BF16 ? hero::kLmBf16 : split ? hero::kLmSplit : hero::kLmF32;
+  const bool mfma = L.mode != hero::kLmF32;
+  const size_t es = L.mode == hero::kLmBf16 ? 2 : split ? 6 : 4;   // bytes of a stored e or g
+  const int ktiles = d.d / 64 * (split ? 6 : 1);
+  // whole tiles of 256 columns whose e (or g) fits the piece, and whose head rows' terms do
   auto fit = [&](size_t rows) {
-    const size_t c = kLmPieceBytes / (es * rows) / 256 * 256;
+    size_t c = kLmPieceBytes / (es * rows);
+    if (split) c = std::min(c, kLmPieceBytes / (6 * w));
     const size_t most = std::min<size_t>((static_cast<size_t>(vocab) + 255) / 256 * 256, kLmHeadRows - 256);
-    return static_cast<int>(std::min(std::max<size_t>(c, 256), most));
+    return static_cast<int>(std::min(std::max<size_t>(c / 256 * 256, 256), most));
   };
   L.chunk = std::min(T, kLmChunk);
   L.n_chunks = (T + L.chunk - 1) / L.chunk;
   L.cols = fit(static_cast<size_t>(L.chunk));
   L.pieces = std::max(1, (vocab - 127 + L.cols - 1) / L.cols);   // no piece of less than two k-tiles
   const int last = vocab - (L.pieces - 1) * L.cols, widest = L.pieces > 1 ? std::max(L.cols, last) : last;
-  L.pitch = up64(widest);
-  L.slices = mfma && dx ? hero::lm_dx_slices(L.chunk, d.d, up64(L.pieces > 1 ? std::min(L.cols, last) : last)) : 1;
+  const int narrowest = L.pieces > 1 ? std::min(L.cols, last) : last;
+  L.pitch = up(widest, 64);
+  L.single = L.pieces == 1 && L.n_chunks == 1;
+  L.keep_e = dx || (dw && L.single);
+  // fp32: the logits are e's buffer
+  L.slices = mfma ? hero::lm_logit_slices(L.chunk, widest, ktiles) : 1;
+  if (mfma && L.slices == 1) L.slices = 0;
+  L.ldl = mfma ? up(widest, 256) : L.pitch;
+  L.dx_depth = up(narrowest, 64) / 64 * (split ? 6 : 1);
+  L.f32_slices = mfma ? 1 : hero::lm_f32_slices(L.chunk, d.d, up(narrowest, 64));
+  const size_t c = static_cast<size_t>(L.chunk);
+  // rows of the accumulators' K slices: up to 256 MiB of them
+  L.acc_rows = !dx ? 0 : mfma ? static_cast<int>(std::max(c, std::min(c * hero::kLmDxSlices, (64u << 20) / w)))
+                              : static_cast<int>(c) * L.f32_slices;
   L.idx = take(t * 4);
   L.inv = take(t * 4);
   L.tgt = take(t * 4);
   L.counts = take((1 + static_cast<size_t>(L.n_chunks)) * 4);
+  L.plan = take(static_cast<size_t>(L.n_chunks) * 4);
+  L.done = take(4);
   L.lt = take(t * 4);
   L.ref = take(t * 4);
   L.sum = take(t * 4);
   L.alpha = take(t * 4);
-  const size_t c = static_cast<size_t>(L.chunk);
-  L.e = take(dx || !mfma ? c * L.pitch * es : 0);
-  L.part = take(mfma ? c * hero::lm_parts(widest) * 8 : 0);
-  L.acc = take(dx ? static_cast<size_t>(L.slices) * c * d.d * 4 : 0);
-  L.g_pitch = std::max(128, up64(T));
-  L.g_cols = fit(static_cast<size_t>(L.g_pitch));
-  L.g_ldl = std::min(L.g_cols, up64(vocab));
-  L.lse = take(dw ? t * 4 : 0);
-  L.own = take(dw ? t * 4 : 0);
+  L.nll = take(t * 4);
+  L.lse = take(t * 4);
+  L.own = take(t * 4);
+  L.e = take(L.keep_e && mfma ? c * L.pitch * es : 0);
+  L.part = take(mfma && !L.slices ? c * hero::lm_parts(widest) * 8 : 0);
+  L.logits = take(L.slices * c * L.ldl * 4);
+  L.acc = take(L.acc_rows * w * 4);
+  L.xs = take(split ? t * w * 6 : 0);
+  L.g_pitch = std::max(128, up(T, 64));
+  L.g_cols = L.single ? vocab : fit(static_cast<size_t>(L.g_pitch));
+  L.g_ldl = up(std::min(L.g_cols, vocab), 64);
+  L.ws = take(split ? std::max<size_t>(widest, dw && !L.single ? std::min(L.g_cols, vocab) : 0) * w * 6 : 0);
+  L.wts = take(split && dx ? static_cast<size_t>(L.pitch) * w * 6 : 0);
   L.g = take(dw ? static_cast<size_t>(std::min(L.g_cols, vocab)) * L.g_pitch * es : 0);
-  L.xT = take(dw ? static_cast<size_t>(d.d) * L.g_pitch * es : 0);
-  L.logits = take(dw && !mfma ? t * L.g_ldl * 4 : 0);
+  L.xT = take(dw ? w * L.g_pitch * es : 0);
+  if (dw && !mfma && !L.single) {   // the logits of all rows, after the loss's are done with
+    const size_t need = t * L.g_ldl * 4;
+    if (need > L.slices * c * L.ldl * 4) L.logits = take(need);
+  }
   L.total = off;
   return L;
 }
@@ -1842,8 +1878,7 @@ int hero_lm_head_weights_make(const hero_dims* dims, int vocab, const void* w, v
   const int pitch = HERO_LM_HEAD_PITCH(vocab);
   if (overlap(w_t, d * pitch * es, w, d * vocab * es)) return HERO_E_ALIAS;
   if ((st = check_device()) != HERO_OK) return st;
-  return hero::launch_transpose(dims->dtype, w, vocab, dims->d, dims->d, w_t, pitch, pitch,
-                                static_cast<hipStream_t>(stream)) == hipSuccess
+  return hero::launch_lm_head(dims->dtype, w, vocab, dims->d, w_t, pitch, static_cast<hipStream_t>(stream)) == hipSuccess
              ? HERO_OK
              : HERO_E_LAUNCH;
 }
@@ -1884,83 +1919,102 @@ int hero_lm_loss(const hero_dims* dims, int vocab, int T, const void* x, const h
   const hipStream_t s = static_cast<hipStream_t>(stream);
   unsigned char* ws = static_cast<unsigned char*>(workspace);
   hero::LmRows a{};
-  a.dtype = D.dtype;
+  a.mode = L.mode;
   a.T = T;
   a.d = D.d;
   a.vocab = vocab;
   a.x = x;
   a.w = head->w;
   a.targets = targets;
-  a.idx = reinterpret_cast<int*>(ws + L.idx);
-  a.inv = reinterpret_cast<int*>(ws + L.inv);
-  a.tgt = reinterpret_cast<int*>(ws + L.tgt);
-  a.counts = reinterpret_cast<int*>(ws + L.counts);
-  a.lt = reinterpret_cast<float*>(ws + L.lt);
-  a.ref = reinterpret_cast<float*>(ws + L.ref);
-  a.sum = reinterpret_cast<float*>(ws + L.sum);
-  a.alpha = reinterpret_cast<float*>(ws + L.alpha);
-  const bool mfma = D.dtype == HERO_BF16, mean = reduction == HERO_LOSS_MEAN;
+  auto ints = [&](size_t at) { return reinterpret_cast<int*>(ws + at); };
+  auto floats = [&](size_t at) { return reinterpret_cast<float*>(ws + at); };
+  a.idx = ints(L.idx);
+  a.inv = ints(L.inv);
+  a.tgt = ints(L.tgt);
+  a.counts = ints(L.counts);
+  a.plan = ints(L.plan);
+  a.done = reinterpret_cast<unsigned*>(ws + L.done);
+  a.lt = floats(L.lt);
+  a.ref = floats(L.ref);
+  a.sum = floats(L.sum);
+  a.alpha = floats(L.alpha);
+  a.nll = floats(L.nll);
+  a.lse = floats(L.lse);
+  a.own = floats(L.own);
+  a.scale = scale;
+  a.mean = reduction == HERO_LOSS_MEAN;
+  a.loss = out->loss;
+  a.token_loss = out->token_loss;
+  a.chunk = L.chunk;
+  a.n_chunks = L.n_chunks;
+  a.dx_tiles = D.d / 256;
+  a.dx_depth = L.dx_depth;
+  a.acc_rows = L.acc_rows;
+  a.f32_slices = L.f32_slices;
+  a.xs = ws + L.xs;
+  const bool mfma = L.mode != hero::kLmF32, split = L.mode == hero::kLmSplit;
+  const float* wf = static_cast<const float*>(head->w);
   hipError_t e = timed(HERO_K_LM_ROWS, s, [&] {
-    const hipError_t y = hero::launch_lm_rows(a, L.chunk, L.n_chunks, s);
-    return y == hipSuccess ? hero::launch_lm_targets(a, s) : y;
+    const hipError_t y = hero::launch_lm_rows(a, s);
+    return y == hipSuccess && split
+               ? hero::launch_lm_terms(static_cast<const float*>(x), D.d, a.idx, a.counts, T, D.d, a.xs, s)
+               : y;
   });
-  hero::LmFinish f{};
-  f.scale = scale;
-  f.mean = mean;
-  f.loss = out->loss;
-  f.token_loss = out->token_loss;
-  f.dx = out->dx;
-  f.lse = dw ? reinterpret_cast<float*>(ws + L.lse) : nullptr;
-  f.own = dw ? reinterpret_cast<float*>(ws + L.own) : nullptr;
-  f.acc = reinterpret_cast<float*>(ws + L.acc);
-  f.slices = L.slices;
+  hero::LmPiece p{};
   for (int c = 0; c < L.n_chunks && e == hipSuccess; ++c) {
-    hero::LmPiece p{};
+    p.chunk = c;
     p.m0 = c * L.chunk;
     p.rows_max = std::min(L.chunk, T - p.m0);
     p.count = a.counts + 1 + c;
-    p.e = dx || !mfma ? ws + L.e : nullptr;
+    p.e = !L.keep_e ? nullptr : mfma ? ws + L.e : ws + L.logits;
     p.part = reinterpret_cast<float2*>(ws + L.part);
-    p.acc = reinterpret_cast<float*>(ws + L.acc);
+    p.logits = L.slices ? floats(L.logits) : nullptr;
     p.slices = L.slices;
+    p.acc = floats(L.acc);
     for (int k = 0; k < L.pieces && e == hipSuccess; ++k) {
       p.v0 = k * L.cols;
       p.cols = lm_piece_cols(L, vocab, k);
       p.pitch = (p.cols + 63) / 64 * 64;
+      p.ldl = mfma ? L.ldl : p.pitch;
       p.first = k == 0;
-      e = timed(HERO_K_LM_LOGITS, s, [&] { return hero::launch_lm_logits(a, p, s); });
+      p.last = k == L.pieces - 1;
+      p.ws = ws + L.ws;
+      p.wts = ws + L.wts;
+      e = timed(HERO_K_LM_LOGITS, s, [&] {
+        const hipError_t y = split ? hero::launch_lm_terms(wf + static_cast<size_t>(p.v0) * D.d, D.d, nullptr, nullptr, p.cols,
+                                                           D.d, ws + L.ws, s)
+                                   : hipSuccess;
+        return y == hipSuccess ? hero::launch_lm_logits(a, p, s) : y;
+      });
       if (e == hipSuccess) e = timed(HERO_K_LM_COMBINE, s, [&] { return hero::launch_lm_combine(a, p, s); });
-      if (e == hipSuccess && dx) e = timed(HERO_K_LM_DX, s, [&] { return hero::launch_lm_dx(a, p, head->w_t, pitch, s); });
+      if (e == hipSuccess && dx)
+        e = timed(HERO_K_LM_DX, s, [&] {
+          const hipError_t y = split ? hero::launch_lm_terms(static_cast<const float*>(head->w_t) + p.v0, pitch, nullptr,
+                                                             nullptr, D.d, p.pitch, ws + L.wts, s)
+                                     : hipSuccess;
+          return y == hipSuccess ? hero::launch_lm_dx(a, p, head->w_t, pitch, s) : y;
+        });
     }
-    f.last = c == L.n_chunks - 1;
-    if (!dx && !f.last) continue;
-    f.m0 = dx ? p.m0 : 0;
-    f.chunk = dx ? p.rows_max : T;
-    if (e == hipSuccess) e = timed(HERO_K_LM_FINISH, s, [&] { return hero::launch_lm_finish(a, f, s); });
+    if (e == hipSuccess && dx) e = timed(HERO_K_LM_FINISH, s, [&] { return hero::launch_lm_finish(a, p, out->dx, s); });
   }
+  if (e == hipSuccess && T > hero::kLmSmall) e = timed(HERO_K_LM_FINISH, s, [&] { return hero::launch_lm_sum(a, s); });
   if (e == hipSuccess && dw)
     e = timed(HERO_K_LM_DW, s, [&] {
       void *g = ws + L.g, *xT = ws + L.xT;
       hipError_t y = hero::launch_lm_xT(a, xT, L.g_pitch, s);
+      if (L.single) {
+        if (y == hipSuccess) y = hero::launch_lm_g_of_e(a, p, g, L.g_pitch, s);
+        return y == hipSuccess ? hero::launch_lm_dw(a, 0, vocab, g, xT, L.g_pitch, out->dw, s) : y;
+      }
       for (int v0 = 0; v0 < vocab && y == hipSuccess; v0 += L.g_cols) {
         const int cols = std::min(L.g_cols, vocab - v0);
-        if (mfma) {
-          y = hero::launch_lm_g(a, v0, cols, f.lse, f.own, g, L.g_pitch, s);
-        } else {
-          float* logits = reinterpret_cast<float*>(ws + L.logits);
-          hero::LmPiece p{};
-          p.rows_max = T;
-          p.v0 = v0;
-          p.cols = cols;
-          p.pitch = L.g_ldl;
-          p.count = a.counts;
-          p.e = logits;
-          y = hero::launch_lm_logits(a, p, s);
-          if (y == hipSuccess)
-            y = hero::launch_lm_g_f32(a, v0, cols, f.lse, f.own, logits, L.g_ldl, scale, mean, static_cast<float*>(g),
-                                      L.g_pitch, s);
-        }
-        if (y == hipSuccess) y = hero::launch_lm_dw(a, v0, cols, g, xT, L.g_pitch, scale, mean, out->dw, s);
+        const float* wv = wf + static_cast<size_t>(v0) * D.d;
+        if (split) y = hero::launch_lm_terms(wv, D.d, nullptr, nullptr, cols, D.d, ws + L.ws, s);
+        if (!mfma)
+          y = hero::launch_lm_f32_logits(static_cast<const float*>(x), a.idx, a.counts, T, wv, cols, D.d, floats(L.logits),
+                                         L.g_ldl, s);
+        if (y == hipSuccess) y = hero::launch_lm_g(a, v0, cols, ws + L.ws, floats(L.logits), L.g_ldl, g, L.g_pitch, s);
+        if (y == hipSuccess) y = hero::launch_lm_dw(a, v0, cols, g, xT, L.g_pitch, out->dw, s);
       }
       return y;
     });

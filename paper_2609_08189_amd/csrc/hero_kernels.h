@@ -400,66 +400,89 @@ hipError_t launch_grad_norm_finish(const double* part, int n, float* norm, hipSt
 hipError_t launch_grad_clip(const GradTable& tab, int groups, const double* part, int n, float max_norm, float* norm,
                             hipStream_t s);
 
-// Language-model loss (k_lm_loss.hip, its products in k_gemm.hip).  Counted tokens are compacted: row
+// Language-model loss (k_lm_loss.hip, its products in k_lm_gemm.hip).  Counted tokens are compacted: row
 // m < counts[0] is token idx[m].
+//   kLmBf16  bf16 model
+//   kLmF32   fp32 model, products in fp32
+//   kLmSplit fp32 model, products of three-term operands on the bf16 matrix cores (SixTerm)
+enum LmMode { kLmBf16 = 0, kLmF32 = 1, kLmSplit = 2 };
+constexpr int kLmDxBlocks = 512, kLmDxSlices = 32;   // a plan of several K slices: most workgroups, most slices
+constexpr int kLmSmall = 1024;   // tokens of a call whose rows are found, and whose losses are added, beside other work
+
 struct LmRows {
-  int dtype, T, d, vocab;
+  int mode, T, d, vocab;
   const void *x, *w;         // [T][d], [vocab][d]
   const int* targets;        // [T]
   int* idx;                  // [T] token of a row
   int* inv;                  // [T] row of a token, or -1
   int* tgt;                  // [T] target of a row
   int* counts;               // [0] all rows; [1 + c] rows of chunk c
+  int* plan;                 // [chunks] tile height of the dx products, K slices << 16
+  unsigned* done;            // rows whose loss is known (at most kLmSmall tokens)
   float* lt;                 // [T] target's logit
   float* ref;                // [T] reference logit of the row's sums
   float* sum;                // [T] sum over the vocabulary but the target of exp(logit - ref)
   float* alpha;              // [T] what the row's earlier sums were last rescaled by
-};
-// counted rows of all tokens, and of each chunk of `chunk` rows
-hipError_t launch_lm_rows(const LmRows& a, int chunk, int n_chunks, hipStream_t s);
-// lt, ref, sum = 0, tgt
-hipError_t launch_lm_targets(const LmRows& a, hipStream_t s);
-
-// One piece of the vocabulary for one chunk of rows: columns [v0, v0 + cols), rows [m0, m0 + rows_max)
-struct LmPiece {
-  int m0, rows_max, v0, cols;
-  int pitch;                 // of e, and of the fp32 logits: cols rounded up to 64
-  const int* count;          // rows of the chunk (device)
-  void* e;                   // [rows_max][pitch] exp(logit - ref) (bf16; fp32: first the logits); null: sums only
-  float2* part;              // bf16: [rows_max][lm_parts(cols)] {reference, sum} of a row's pieces
-  float* acc;                // [slices][rows_max][d] sum over the vocabulary of e W
-  int slices;
-  bool first;                // acc is written, not added to
-};
-int lm_parts(int cols);
-int lm_dx_slices(int rows_max, int d, int depth);
-hipError_t launch_lm_logits(const LmRows& a, const LmPiece& p, hipStream_t s);
-// the row's sums with this piece's; e in units of the row's reference after it
-hipError_t launch_lm_combine(const LmRows& a, const LmPiece& p, hipStream_t s);
-hipError_t launch_lm_dx(const LmRows& a, const LmPiece& p, const void* w_t, int ld_wt, hipStream_t s);
-
-struct LmFinish {
-  int m0, chunk, slices;     // rows [m0, m0 + chunk) are complete
-  bool last;                 // no chunk after this one: the loss, and the tokens that do not count
-  const float* acc;          // [slices][chunk][d]
+  float* nll;                // [T]
+  float *lse, *own;          // [T] log sum of a row's logits, p - 1 of its target
   float scale;
   bool mean;
   float *loss, *token_loss;  // token_loss may be null
-  void* dx;                  // null: none wanted
-  float *lse, *own;          // [T] of a row for dW: log sum of its logits, p - 1 of its target; null: none wanted
+  // chunks of rows, and what the dx products' plan goes by: column tiles, k-tiles, rows of the accumulators
+  int chunk, n_chunks, dx_tiles, dx_depth, acc_rows;
+  int f32_slices;            // kLmF32: K slices
+  void* xs;                  // kLmSplit: [3][T][d] the rows' terms
 };
-hipError_t launch_lm_finish(const LmRows& a, const LmFinish& f, hipStream_t s);
+// the rows, their targets' logits; everything else that a call starts from
+hipError_t launch_lm_rows(const LmRows& a, hipStream_t s);
+// loss[0] of more than kLmSmall tokens (of fewer: the last combine)
+hipError_t launch_lm_sum(const LmRows& a, hipStream_t s);
 
-// dW of the columns [v0, v0 + cols), all rows at once.  g [cols][pitch]: the loss's gradient over the logits, the
-// rows contiguous, zero behind the last; xT [d][pitch]: the counted rows of x, transposed, zero likewise.
-// bf16: launch_lm_g forms the logits anew and leaves the unit scale / N to launch_lm_dw; fp32: launch_lm_g_f32 from the
-// logits [T][ldl] of launch_lm_logits, unit included.
+// One piece of the vocabulary for one chunk of rows: columns [v0, v0 + cols), rows [m0, m0 + rows_max)
+struct LmPiece {
+  int chunk, m0, rows_max, v0, cols;
+  int pitch;                 // of e: cols rounded up to 64
+  bool first, last;          // of the pieces
+  const int* count;          // rows of the chunk (device)
+  void* e;                   // [rows_max][pitch] exp(logit - ref), zero at the target (kLmSplit: three arrays); may be null
+  float2* part;              // [rows_max][lm_parts(cols)] {reference, sum} of a row's 64-column pieces
+  float* logits;             // [slices][rows_max][ldl] partial logits instead of e and part; null: none
+  int slices, ldl;
+  const void* ws;            // kLmSplit: [3][cols][d] terms of the piece's head rows
+  const void* wts;           // kLmSplit: [3][d][pitch] ... transposed
+  float* acc;                // [slices of the plan][rows][d] sum over the vocabulary of e W
+};
+int lm_parts(int cols);
+int lm_logit_slices(int rows, int cols, int ktiles);
+hipError_t launch_lm_logits(const LmRows& a, const LmPiece& p, hipStream_t s);
+// the row's sums with this piece's; e in units of the row's reference after it; after the last piece its loss
+hipError_t launch_lm_combine(const LmRows& a, const LmPiece& p, hipStream_t s);
+hipError_t launch_lm_dx(const LmRows& a, const LmPiece& p, const void* w_t, int ld_wt, hipStream_t s);
+// dx of the chunk's tokens (with the last chunk: zeros of the tokens that do not count)
+hipError_t launch_lm_finish(const LmRows& a, const LmPiece& p, void* dx, hipStream_t s);
+// kLmF32, in k_gemm.hip
+hipError_t launch_lm_f32_logits(const float* x, const int* idx, const int* count, int rows_max, const float* w, int cols,
+                                int d, float* out, int ldl, hipStream_t s);
+hipError_t launch_lm_f32_dx(const float* e, const int* count, int rows_max, int pitch, const float* w_t, int ld_wt, int d,
+                            int slices, const float* alpha, bool first, float* acc, hipStream_t s);
+hipError_t launch_lm_f32_dw(const float* g, int cols, const float* xT, int d, int pitch, float* dw, hipStream_t s);
+int lm_f32_slices(int rows, int d, int K);
+
+// dW of the columns [v0, v0 + cols), all rows at once.  g [cols][pitch]: p - [target] (kLmF32: times the
+// unit, scale / N), the rows contiguous, zero behind the last; xT [d][pitch]: the counted rows of x,
+// transposed, zero likewise (kLmSplit: three arrays each).
 hipError_t launch_lm_xT(const LmRows& a, void* xT, int pitch, hipStream_t s);
-hipError_t launch_lm_g(const LmRows& a, int v0, int cols, const float* lse, const float* own, void* g, int pitch,
+// g from the logits formed anew (kLmF32: given, [rows][ldl])
+hipError_t launch_lm_g(const LmRows& a, int v0, int cols, const void* ws, const float* logits, int ldl, void* g, int pitch,
                        hipStream_t s);
-hipError_t launch_lm_g_f32(const LmRows& a, int v0, int cols, const float* lse, const float* own, const float* logits,
-                           int ldl, float scale, bool mean, float* g, int pitch, hipStream_t s);
-hipError_t launch_lm_dw(const LmRows& a, int v0, int cols, const void* g, const void* xT, int pitch, float scale, bool mean,
-                        void* dw, hipStream_t s);
+hipError_t launch_lm_g_products(const LmRows& a, int v0, int cols, const void* ws, void* g, int pitch, hipStream_t s);
+// g from the e of a call of one piece and one chunk
+hipError_t launch_lm_g_of_e(const LmRows& a, const LmPiece& p, void* g, int pitch, hipStream_t s);
+hipError_t launch_lm_dw(const LmRows& a, int v0, int cols, const void* g, const void* xT, int pitch, void* dw, hipStream_t s);
+
+// out[t][r][c], t < 3: the terms of in[r][c] (row idx[r] where given, *count rows); cols a multiple of 8
+hipError_t launch_lm_terms(const float* in, int ld_in, const int* idx, const int* count, int rows, int cols, void* out,
+                           hipStream_t s);
+hipError_t launch_lm_head(int dtype, const void* w, int vocab, int d, void* w_t, int pitch, hipStream_t s);
 
 }  // namespace hero

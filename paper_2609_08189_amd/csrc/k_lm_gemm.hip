@@ -1,0 +1,334 @@
+// The products of the language-model loss over one piece of the vocabulary (k_lm_loss.hip has the formulas):
+//   logits   l = x[idx] W^T        -> e = exp(l - ref) as stored, and its sums a row and 64 columns; few
+//                                     tiles: K slices of l in fp32, which the combining pass turns into e
+//   dx       acc (+)= e W          B = W^T [d][pitch of the vocabulary]
+//   dW       g = (p - [target])^T  = W x^T with an epilogue, the tokens contiguous
+//            dW = unit g x         B = x^T [d][tokens]
+// All on the phase-ordered core, whose rate on random operands (1.3 to 1.45 PFLOP/s) bounds them.  fp32 models: the
+// same products on three-term operands (kLmSplit).
+#include "hero_gemm.h"
+
+#include "hero_kernels.h"
+
+namespace hero {
+namespace {
+
+// Where a logit may stand above its row's reference before the piece takes one of its own: e stays far
+// from the end of the range (e^60 summed over any vocabulary, times any weight, is below 2^120).
+constexpr float kLmAbove = 60.0f;
+
+template <bool SIX>
+struct Six {};
+template <>
+struct Six<true> {
+  static constexpr bool kSixTerm = true;
+};
+
+// eight values as stored: bf16, or three bf16 terms `term` elements apart
+template <bool SIX>
+__device__ __forceinline__ void st8_terms(bf16_t* p, size_t term, const float* v) {
+  if constexpr (!SIX) {
+    st8(p, v);
+  } else {
+    float r[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) r[k] = v[k];
+#pragma unroll
+    for (int t = 0; t < 3; ++t) {
+      st8(p + t * term, r);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) r[k] -= bf16_to_f32(f32_to_bf16(r[k]));
+    }
+  }
+}
+
+template <bool SIX>
+__device__ __forceinline__ float lm_exp(float x) {
+  return SIX ? expf(x) : __expf(x);
+}
+
+// e[m][n] = exp(l - ref_m) for every column but the target's, whose share is kept apart (1 - p of a sure
+// token would cancel in it).  ref is the target's logit, or what the row's earlier pieces raised it to, so
+// no pass for a maximum is needed: e is a floating number whatever its size.  Where a logit is more than
+// kLmAbove over it, the wave's 64 columns of that row take their own maximum as reference, and the pass
+// over the partial sums brings them together.  The 64 columns of a row sit in eight neighbouring lanes.
+template <bool STORE, bool SIX>
+struct EpiLmExp : Six<SIX> {
+  const float* ref;
+  const int* tgt;
+  int v0, cols, pitch;
+  bf16_t* e;
+  size_t term;
+  float2* part;
+  int parts;
+  struct Pre {
+    float ref;
+    int tgt;
+  };
+  __device__ __forceinline__ Pre prep(int m, int) const { return {ref[m], tgt[m] - v0}; }
+  __device__ __forceinline__ void emit8(const Pre& p, int m, int n, const float* v) const {
+    float x[8], s = 0.f;
+    float mx = v[0];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      x[k] = v[k];
+      mx = fmaxf(mx, x[k]);
+    }
+    float r = p.ref;
+    // all lanes inside the vocabulary, away from their targets and their references good: the plain case
+    const bool plain = n + 8 <= cols && static_cast<unsigned>(p.tgt - n) >= 8u && !(mx - r > kLmAbove);
+    if (__all(plain)) {
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        x[k] = lm_exp<SIX>(x[k] - r);
+        s += x[k];
+      }
+    } else {
+      mx = r;
+#pragma unroll
+      for (int k = 0; k < 8; ++k)
+        if (n + k < cols) mx = fmaxf(mx, x[k]);
+      mx = fmaxf(mx, __shfl_xor(mx, 1, 8));
+      mx = fmaxf(mx, __shfl_xor(mx, 2, 8));
+      mx = fmaxf(mx, __shfl_xor(mx, 4, 8));
+      if (mx - r > kLmAbove) r = mx;
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        x[k] = n + k < cols && n + k != p.tgt ? lm_exp<SIX>(x[k] - r) : 0.f;
+        s += x[k];
+      }
+    }
+    if constexpr (STORE) {
+      if (n < pitch) st8_terms<SIX>(e + static_cast<size_t>(m) * pitch + n, term, x);
+    }
+    s = group_sum<8>(s);
+    if ((threadIdx.x & 7) == 0) part[static_cast<size_t>(m) * parts + (n >> 8) * 4 + ((n & 127) >> 5)] = {r, s};
+  }
+};
+
+template <bool SIX>
+struct EpiLmLogits : EpiStoreF32, Six<SIX> {};
+
+// acc[m][n] = the piece's product, or alpha_m acc[m][n] + it
+template <bool FIRST, bool SIX>
+struct EpiLmAcc : Six<SIX> {
+  float* out;
+  int ld;
+  const float* alpha;
+  struct Pre {
+    f32x4 o[FIRST ? 1 : 2];
+    float a;
+  };
+  __device__ __forceinline__ float* at(int m, int n) const { return out + static_cast<size_t>(m) * ld + n; }
+  __device__ __forceinline__ Pre prep(int m, int n) const {
+    Pre p{};
+    if constexpr (!FIRST) {
+      p.o[0] = *reinterpret_cast<const f32x4*>(at(m, n));
+      p.o[1] = *reinterpret_cast<const f32x4*>(at(m, n) + 4);
+      p.a = alpha[m];
+    }
+    return p;
+  }
+  __device__ __forceinline__ void emit8(const Pre& p, int m, int n, const float* v) const {
+    f32x4 lo = *reinterpret_cast<const f32x4*>(v), hi = *reinterpret_cast<const f32x4*>(v + 4);
+    if constexpr (!FIRST) {
+      lo += p.a * p.o[0];
+      hi += p.a * p.o[1];
+    }
+    *reinterpret_cast<f32x4*>(at(m, n)) = lo;
+    *reinterpret_cast<f32x4*>(at(m, n) + 4) = hi;
+  }
+};
+
+// columns of the tokens that a product over them as K runs through: at least two k-tiles
+__device__ __forceinline__ int lm_depth(const int* count) { return max(2 * BK, (*count + BK - 1) / BK * BK); }
+
+// g[v][t] = p_tv - [v = target of t] for the counted rows t, zero behind them (the unit, scale / N, is
+// dW's epilogue's); columns: the tokens' log sums and targets
+template <bool SIX>
+struct EpiLmG : Six<SIX> {
+  static constexpr bool kColumns = true;
+  const float *lse, *own;    // [rows] log sum of a row, p - 1 of its target
+  const int *tgt, *count;
+  int v0, pitch;
+  bf16_t* g;
+  size_t term;
+  struct Cols {
+    float lse[8];
+    int tgt[8];
+  };
+  struct Pre {};
+  __device__ __forceinline__ Pre prep(int, int) const { return {}; }
+  __device__ __forceinline__ bool skip(int n0) const { return n0 >= lm_depth(count); }
+  __device__ __forceinline__ Cols cols(int n) const {
+    Cols c;
+    const int N = *count;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const bool in = n + k < N;
+      c.lse[k] = in ? lse[n + k] : 0.f;
+      c.tgt[k] = in ? tgt[n + k] - v0 : INT_MIN;
+    }
+    return c;
+  }
+  __device__ __forceinline__ void emit8(const Cols& c, int m, int n, const float* v) const {
+    if (n >= pitch) return;
+    float x[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      x[k] = c.tgt[k] == INT_MIN ? 0.f : lm_exp<SIX>(v[k] - c.lse[k]);
+      if (c.tgt[k] == m) x[k] = own[n + k];
+    }
+    st8_terms<SIX>(g + static_cast<size_t>(m) * pitch + n, term, x);
+  }
+};
+
+template <typename T, bool SIX>
+struct EpiLmDw : Six<SIX> {   // dw[m][n] = unit acc, the tokens as K
+  static constexpr bool kDeviceDepth = true;
+  T* out;
+  int ld;
+  const int* count;
+  float scale;
+  bool mean;
+  struct Pre {
+    float c;
+  };
+  __device__ __forceinline__ int depth() const { return lm_depth(count); }
+  __device__ __forceinline__ Pre prep(int, int) const { return {mean ? scale / static_cast<float>(max(*count, 1)) : scale}; }
+  __device__ __forceinline__ void emit8(const Pre& p, int m, int n, const float* v) const {
+    float x[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) x[k] = p.c * v[k];
+    st8(out + static_cast<size_t>(m) * ld + n, x);
+  }
+};
+
+// The dx product on the tile height and K slices that the rows' plan names; slice z into acc + z M d.
+// The grid covers any plan: the workgroups of a slice come one after another, a multiple of eight, so
+// that each XCD keeps its share of every slice's tile order.
+template <class Epi>
+__global__ __launch_bounds__(512, 2) void lm_dx_kernel(ARows<bf16_t> A, BRows<bf16_t> B, Epi epi,
+                                                       const int* __restrict__ m_count, const int* __restrict__ plan,
+                                                       int M_max, int K, int n_tiles) {
+  __shared__ __attribute__((aligned(1024))) unsigned char smem[2 * Phase<256, false>::STAGE];
+  const int M = min(*m_count, M_max), bm = *plan & 0xffff, S = *plan >> 16;
+  const int per = ((M + bm - 1) / bm * n_tiles + 7) / 8 * 8;
+  if (per == 0) return;
+  const int z = static_cast<int>(blockIdx.x) / per, bid = static_cast<int>(blockIdx.x) % per;
+  if (z >= S) return;
+  epi.out += static_cast<size_t>(z) * M * epi.ld;
+  if (bm == 256)
+    phase_tile<Phase<256, false>>(A, B, epi, M, M_max, K, n_tiles, smem, bid, z, S);
+  else if (bm == 192)
+    phase_tile<Phase<192, false>>(A, B, epi, M, M_max, K, n_tiles, smem, bid, z, S);
+  else
+    phase_tile<Phase<128, false>>(A, B, epi, M, M_max, K, n_tiles, smem, bid, z, S);
+}
+
+int lm_tiles(int n) { return (n + 255) / 256; }
+
+template <bool SIX>
+hipError_t lm_logits(const LmRows& a, const LmPiece& p, hipStream_t s) {
+  const int n = lm_tiles(p.cols) * 256;
+  ARows<bf16_t> A{static_cast<const bf16_t*>(a.x), a.idx + p.m0, a.d};
+  BRows<bf16_t> B{static_cast<const bf16_t*>(a.w) + static_cast<size_t>(p.v0) * a.d, nullptr, INT_MAX, a.d, p.cols - 1};
+  if constexpr (SIX) {
+    A = {static_cast<const bf16_t*>(a.xs) + static_cast<size_t>(p.m0) * a.d, nullptr, a.d, nullptr, a.d / BK,
+         static_cast<size_t>(a.T) * a.d};
+    B.b0 = static_cast<const bf16_t*>(p.ws);
+    B.term = static_cast<size_t>(p.cols) * a.d;
+  }
+  const int K = SIX ? 6 * a.d : a.d;
+  if (p.logits) {
+    const EpiLmLogits<SIX> epi{{p.logits, p.ldl, static_cast<size_t>(p.rows_max) * p.ldl}, {}};
+    return run_phase_split(A, B, epi, p.count, p.rows_max, n, K, p.slices, s);
+  }
+  const float* ref = a.ref + p.m0;
+  const int* tgt = a.tgt + p.m0;
+  bf16_t* e = static_cast<bf16_t*>(p.e);
+  const size_t term = static_cast<size_t>(p.rows_max) * p.pitch;
+  const int parts = lm_parts(p.cols);
+  if (e)
+    return run_phase<false>(A, B, EpiLmExp<true, SIX>{{}, ref, tgt, p.v0, p.cols, p.pitch, e, term, p.part, parts}, p.count,
+                            p.rows_max, n, K, s, false);
+  return run_phase<false>(A, B, EpiLmExp<false, SIX>{{}, ref, tgt, p.v0, p.cols, p.pitch, e, term, p.part, parts}, p.count,
+                          p.rows_max, n, K, s, false);
+}
+
+template <bool SIX>
+hipError_t lm_dx(const LmRows& a, const LmPiece& p, const void* w_t, int ld_wt, hipStream_t s) {
+  ARows<bf16_t> A{static_cast<const bf16_t*>(p.e), nullptr, p.pitch, nullptr, p.pitch / BK,
+                  static_cast<size_t>(p.rows_max) * p.pitch};
+  BRows<bf16_t> B{static_cast<const bf16_t*>(w_t) + p.v0, nullptr, INT_MAX, ld_wt};
+  if constexpr (SIX) B = {static_cast<const bf16_t*>(p.wts), nullptr, INT_MAX, p.pitch, INT_MAX, nullptr,
+                          static_cast<size_t>(a.d) * p.pitch};
+  const int n_tiles = a.d / 256, K = SIX ? 6 * p.pitch : p.pitch;
+  const int blocks = std::max((p.rows_max + 127) / 128 * n_tiles, kLmDxBlocks) + 8 * kLmDxSlices;
+  const float* alpha = a.alpha + p.m0;
+  const int* plan = a.plan + p.chunk;
+  if (p.first)
+    lm_dx_kernel<<<blocks, 512, 0, s>>>(A, B, EpiLmAcc<true, SIX>{{}, p.acc, a.d, alpha}, p.count, plan, p.rows_max, K, n_tiles);
+  else
+    lm_dx_kernel<<<blocks, 512, 0, s>>>(A, B, EpiLmAcc<false, SIX>{{}, p.acc, a.d, alpha}, p.count, plan, p.rows_max, K, n_tiles);
+  return hipGetLastError();
+}
+
+template <bool SIX>
+hipError_t lm_g(const LmRows& a, int v0, int cols, const void* ws, void* g, int pitch, hipStream_t s) {
+  ARows<bf16_t> A{static_cast<const bf16_t*>(a.w) + static_cast<size_t>(v0) * a.d, nullptr, a.d};
+  BRows<bf16_t> B{static_cast<const bf16_t*>(a.x), nullptr, INT_MAX, a.d, a.T - 1, a.idx};
+  if constexpr (SIX) {
+    A = {static_cast<const bf16_t*>(ws), nullptr, a.d, nullptr, a.d / BK, static_cast<size_t>(cols) * a.d};
+    B = {static_cast<const bf16_t*>(a.xs), nullptr, INT_MAX, a.d, a.T - 1, nullptr, static_cast<size_t>(a.T) * a.d};
+  }
+  const EpiLmG<SIX> epi{{}, a.lse, a.own, a.tgt, a.counts, v0, pitch, static_cast<bf16_t*>(g), static_cast<size_t>(cols) * pitch};
+  return run_phase<false>(A, B, epi, nullptr, cols, lm_tiles(pitch) * 256, SIX ? 6 * a.d : a.d, s);
+}
+
+template <typename T, bool SIX>
+hipError_t lm_dw(const LmRows& a, int v0, int cols, const void* g, const void* xT, int pitch, void* dw, hipStream_t s) {
+  ARows<bf16_t> A{static_cast<const bf16_t*>(g), nullptr, pitch, nullptr, 0, static_cast<size_t>(cols) * pitch};
+  BRows<bf16_t> B{static_cast<const bf16_t*>(xT), nullptr, INT_MAX, pitch, INT_MAX, nullptr, static_cast<size_t>(a.d) * pitch};
+  const EpiLmDw<T, SIX> epi{{}, static_cast<T*>(dw) + static_cast<size_t>(v0) * a.d, a.d, a.counts, a.scale, a.mean};
+  return run_phase<false>(A, B, epi, nullptr, cols, a.d, pitch, s);
+}
+
+}  // namespace
+
+int lm_parts(int cols) { return 4 * lm_tiles(cols); }
+
+// K slices of the logits where 128-row tiles leave half of the CUs idle or more, at least four k-tiles each, unless
+// the rows are long: one workgroup takes a row of them to its exponentials (one row of 32000: 26 us, with the
+// epilogue's exponentials 5)
+int lm_logit_slices(int rows, int cols, int ktiles) {
+  const int tiles = (rows + 127) / 128 * lm_tiles(cols);
+  return 2 * tiles > kCUs || cols > 8192 ? 1 : std::max(1, std::min(kCUs / tiles, ktiles / 4));
+}
+
+hipError_t launch_lm_logits(const LmRows& a, const LmPiece& p, hipStream_t s) {
+  if (a.mode == kLmBf16) return lm_logits<false>(a, p, s);
+  if (a.mode == kLmSplit) return lm_logits<true>(a, p, s);
+  return launch_lm_f32_logits(static_cast<const float*>(a.x), a.idx + p.m0, p.count, p.rows_max,
+                              static_cast<const float*>(a.w) + static_cast<size_t>(p.v0) * a.d, p.cols, a.d, p.logits, p.ldl, s);
+}
+
+hipError_t launch_lm_dx(const LmRows& a, const LmPiece& p, const void* w_t, int ld_wt, hipStream_t s) {
+  if (a.mode == kLmBf16) return lm_dx<false>(a, p, w_t, ld_wt, s);
+  if (a.mode == kLmSplit) return lm_dx<true>(a, p, nullptr, 0, s);
+  return launch_lm_f32_dx(static_cast<const float*>(p.e), p.count, p.rows_max, p.pitch, static_cast<const float*>(w_t) + p.v0,
+                          ld_wt, a.d, a.f32_slices, a.alpha + p.m0, p.first, p.acc, s);
+}
+
+hipError_t launch_lm_dw(const LmRows& a, int v0, int cols, const void* g, const void* xT, int pitch, void* dw, hipStream_t s) {
+  if (a.mode == kLmBf16) return lm_dw<bf16_t, false>(a, v0, cols, g, xT, pitch, dw, s);
+  if (a.mode == kLmSplit) return lm_dw<float, true>(a, v0, cols, g, xT, pitch, dw, s);
+  return launch_lm_f32_dw(static_cast<const float*>(g), cols, static_cast<const float*>(xT), a.d, pitch,
+                          static_cast<float*>(dw) + static_cast<size_t>(v0) * a.d, s);
+}
+
+hipError_t launch_lm_g_products(const LmRows& a, int v0, int cols, const void* ws, void* g, int pitch, hipStream_t s) {
+  return a.mode == kLmSplit ? lm_g<true>(a, v0, cols, ws, g, pitch, s) : lm_g<false>(a, v0, cols, ws, g, pitch, s);
+}
+
+}  // namespace hero

@@ -9,11 +9,11 @@
 // is a difference of close numbers.  The target's logit, found by a dot product before anything else,
 // is the reference of all exponentials, which is why one pass over the vocabulary is enough: a row's sums
 // and its sum of e W are gathered piece by piece and divided at the end.  A row whose logits rise more
-// than e^60 above its target changes its reference on the way (EpiLmExp, lm_combine_kernel).
+// than e^60 above its target changes its reference on the way (EpiLmExp, the combining pass).
 //
 // Tokens without a target cost nothing: the rows that count are compacted on the device, and every product
-// takes their number from there.  The passes here are a row or a token a wave and read what the products
-// left in the last-level cache; the products (k_gemm.hip) bound the whole.
+// takes their number from there.  The passes here are short and read what the products left in the caches;
+// the products (k_lm_gemm.hip) bound the whole, launches and latencies the smallest calls.
 #include <limits.h>
 
 #include <algorithm>
@@ -26,43 +26,53 @@ namespace {
 
 constexpr int kRowsThreads = 1024;
 
-// Ordered compaction by one workgroup, a run of neighbouring tokens per thread.
-__global__ __launch_bounds__(kRowsThreads) void lm_rows_kernel(LmRows a, int chunk, int n_chunks) {
-  __shared__ int wsum[kRowsThreads / kWave];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int per = (a.T + kRowsThreads - 1) / kRowsThreads;
-  const int t0 = min(a.T, static_cast<int>(threadIdx.x) * per), t1 = min(a.T, t0 + per);
-  int n = 0;
-  for (int t = t0; t < t1; ++t) n += static_cast<unsigned>(a.targets[t]) < static_cast<unsigned>(a.vocab);
-  int incl = n;
-#pragma unroll
-  for (int off = 1; off < kWave; off <<= 1) {
-    const int v = __shfl_up(incl, off, kWave);
-    if (lane >= off) incl += v;
-  }
-  if (lane == 63) wsum[wave] = incl;
-  __syncthreads();
-  int m = incl - n, total = 0;
-  for (int w = 0; w < kRowsThreads / kWave; ++w) {
-    if (w < wave) m += wsum[w];
-    total += wsum[w];
-  }
-  for (int t = t0; t < t1; ++t) {
-    const bool in = static_cast<unsigned>(a.targets[t]) < static_cast<unsigned>(a.vocab);
-    a.inv[t] = in ? m : -1;
-    if (in) a.idx[m++] = t;
-  }
-  for (int i = total + threadIdx.x; i < a.T; i += kRowsThreads) a.idx[i] = 0;   // rows that no result uses
-  if (threadIdx.x == 0) a.counts[0] = total;
-  for (int c = threadIdx.x; c < n_chunks; c += kRowsThreads) a.counts[1 + c] = max(0, min(chunk, total - c * chunk));
+__device__ __forceinline__ bool counts_of(const LmRows& a, int t) {
+  return static_cast<unsigned>(a.targets[t]) < static_cast<unsigned>(a.vocab);
 }
 
-// The target's logit, a wave a row
+// Tile height and K slices of the dx products of M rows, by one wave, a candidate a lane and turn: the time in
+// rounds of workgroups over the CUs, a round weighted by its height (as phase_rows) and by its k-tiles, of which
+// storing an fp32 tile takes about twelve, and the finishing pass's reading of all slices (125 is a k-tile of 256
+// rows, 1.45 us).  2048 rows of d = 4096 against 32768 columns: 128-row tiles in one round 443 us, 256-row tiles in
+// two slices 399.
+__device__ __forceinline__ int dx_plan(const LmRows& a, int M, int lane) {
+  float time = 3.0e38f;
+  int best = 256 | 1 << 16;
+  for (int c = lane; c < 3 * kLmDxSlices; c += kWave) {
+    const int bm = 256 - 64 * (c % 3), S = 1 + c / 3, w = bm == 256 ? 125 : bm == 192 ? 100 : 75;
+    const int tiles = (M + bm - 1) / bm * a.dx_tiles;
+    if (S > 1 && (static_cast<long long>(S) * M > a.acc_rows || tiles * S > kLmDxBlocks || a.dx_depth < 4 * S)) continue;
+    const float v = static_cast<float>((tiles * S + 255) / 256 * w) * (static_cast<float>(a.dx_depth) / S + 12.f) +
+                    static_cast<float>(S) * M * a.d * (125.f * 4.f / (1.45f * 4.0e6f));
+    if (v < time) {
+      time = v;
+      best = bm | S << 16;
+    }
+  }
+#pragma unroll
+  for (int off = 32; off > 0; off >>= 1) {
+    const float v = __shfl_xor(time, off, kWave);
+    const int b = __shfl_xor(best, off, kWave);
+    if (v < time || (v == time && b < best)) {
+      time = v;
+      best = b;
+    }
+  }
+  return best;
+}
+
+__device__ __forceinline__ void write_plan(const LmRows& a, int c, int rows, int lane) {
+  const int plan = a.mode == kLmF32 ? 128 | a.f32_slices << 16 : a.acc_rows == 0 ? 0 : dx_plan(a, rows, lane);
+  if (lane == 0) {
+    a.counts[1 + c] = rows;
+    a.plan[c] = plan;
+  }
+}
+
+// The target's logit of row m, token t, by one wave
 template <typename T>
-__global__ __launch_bounds__(256) void lm_targets_kernel(LmRows a) {
-  const int lane = threadIdx.x & 63, m = blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (m >= a.counts[0]) return;
-  const int t = a.idx[m], y = a.targets[t];
+__device__ __forceinline__ void target_row(const LmRows& a, int m, int t, int lane) {
+  const int y = a.targets[t];
   const T* x = static_cast<const T*>(a.x) + static_cast<size_t>(t) * a.d;
   const T* w = static_cast<const T*>(a.w) + static_cast<size_t>(y) * a.d;
   float s = 0.f;
@@ -83,221 +93,540 @@ __global__ __launch_bounds__(256) void lm_targets_kernel(LmRows a) {
   }
 }
 
-// The sums of a row's pieces of 64 columns, a wave a row.  A piece whose reference is not the row's (a logit
-// far above the target's) raises the row's: then the earlier sums, and this piece's e, are rescaled.
-__global__ __launch_bounds__(256) void lm_combine_kernel(LmRows a, LmPiece p, int parts) {
-  const int lane = threadIdx.x & 63, i = blockIdx.x * 4 + (threadIdx.x >> 6), m = p.m0 + i;
-  if (i >= *p.count) return;
-  const float r0 = a.ref[m];
-  const float2* part = p.part + static_cast<size_t>(i) * parts;
-  float s = 0.f, r = r0;
-  for (int q = lane; q < parts; q += kWave) r = fmaxf(r, part[q].x);
+// Up to kLmSmall tokens in one launch: every workgroup counts all targets for itself, four a thread, and
+// takes the four tokens of one of its threads, a wave each.
+template <typename T>
+__global__ __launch_bounds__(256) void lm_rows_small_kernel(LmRows a) {
+  __shared__ int wsum[4], rank[4], live[4];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, t0 = 4 * threadIdx.x;
+  int in[4], n = 0;
 #pragma unroll
-  for (int off = 32; off > 0; off >>= 1) r = fmaxf(r, __shfl_xor(r, off, kWave));
-  const bool raised = r > r0;
-  for (int q = lane; q < parts; q += kWave) {
-    const float2 v = part[q];
-    s += raised ? v.y * __expf(v.x - r) : v.y;
+  for (int k = 0; k < 4; ++k) {
+    in[k] = t0 + k < a.T && counts_of(a, t0 + k);
+    n += in[k];
   }
-  s = wave_sum(s);
-  const float f0 = raised ? __expf(r0 - r) : 1.0f;
+  int incl = n;
+#pragma unroll
+  for (int off = 1; off < kWave; off <<= 1) {
+    const int v = __shfl_up(incl, off, kWave);
+    if (lane >= off) incl += v;
+  }
+  if (lane == 63) wsum[wave] = incl;
+  __syncthreads();
+  const int total = wsum[0] + wsum[1] + wsum[2] + wsum[3];
+  if (threadIdx.x == blockIdx.x) {
+    int m = incl - n;
+    for (int w = 0; w < wave; ++w) m += wsum[w];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      live[k] = in[k];
+      rank[k] = m;
+      m += in[k];
+    }
+  }
+  if (blockIdx.x == 0) {
+    if (wave == 3) {
+      if (lane == 0) {
+        a.counts[0] = total;
+        *a.done = 0;
+      }
+      write_plan(a, 0, total, lane);
+    }
+    for (int i = total + threadIdx.x; i < a.T; i += 256) a.idx[i] = 0;   // rows that no result uses
+  }
+  __syncthreads();
+  const int t = 4 * blockIdx.x + wave, m = rank[wave];
+  if (t >= a.T) return;
+  if (!live[wave]) {
+    if (lane == 0) {
+      a.inv[t] = -1;
+      if (a.token_loss) a.token_loss[t] = 0.f;
+    }
+    return;
+  }
   if (lane == 0) {
-    a.sum[m] = fmaf(a.sum[m], f0, s);
-    a.alpha[m] = f0;
-    a.ref[m] = r;
+    a.inv[t] = m;
+    a.idx[m] = t;
   }
-  if (!raised || !p.e) return;
-  bf16_t* e = static_cast<bf16_t*>(p.e) + static_cast<size_t>(i) * p.pitch;
-  for (int n = lane; n < p.pitch; n += kWave) {   // the columns of wave q of tile n / 256: (n & 127) / 32
-    const float f = __expf(part[(n >> 8) * 4 + ((n & 127) >> 5)].x - r);
-    e[n] = f32_to_bf16(bf16_to_f32(e[n]) * f);
-  }
+  target_row<T>(a, m, t, lane);
 }
 
-// fp32: the logits of a piece to e, in place, a workgroup a row; with zeros up to the pitch
-__global__ __launch_bounds__(256) void lm_exp_f32_kernel(LmRows a, LmPiece p) {
-  __shared__ float red[4];
-  const int i = blockIdx.x, m = p.m0 + i, wave = threadIdx.x >> 6;
-  if (i >= *p.count) return;
-  const float r0 = a.ref[m];
-  const int tgt = a.tgt[m] - p.v0;
-  float* e = static_cast<float*>(p.e) + static_cast<size_t>(i) * p.pitch;
-  float r = r0;
-  for (int n = threadIdx.x; n < p.cols; n += 256) r = fmaxf(r, e[n]);
+// More tokens: ordered compaction by one workgroup, a run of neighbouring tokens per thread, then a wave a row.
+__global__ __launch_bounds__(kRowsThreads) void lm_rows_kernel(LmRows a) {
+  __shared__ int wsum[kRowsThreads / kWave];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int per = (a.T + kRowsThreads - 1) / kRowsThreads;
+  const int t0 = min(a.T, static_cast<int>(threadIdx.x) * per), t1 = min(a.T, t0 + per);
+  int n = 0;
+  for (int t = t0; t < t1; ++t) n += counts_of(a, t);
+  int incl = n;
 #pragma unroll
-  for (int off = 32; off > 0; off >>= 1) r = fmaxf(r, __shfl_xor(r, off, kWave));
-  if ((threadIdx.x & 63) == 0) red[wave] = r;
-  __syncthreads();
-  r = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
-  __syncthreads();
-  // the target's logit is a good reference unless the row rises far above it
-  if (!(r - r0 > 60.0f)) r = r0;
-  float s = 0.f;
-  for (int n = threadIdx.x; n < p.pitch; n += 256) {
-    const float v = n < p.cols && n != tgt ? expf(e[n] - r) : 0.f;
-    e[n] = v;
-    s += v;
+  for (int off = 1; off < kWave; off <<= 1) {
+    const int v = __shfl_up(incl, off, kWave);
+    if (lane >= off) incl += v;
   }
-  s = wave_sum(s);
-  if ((threadIdx.x & 63) == 0) red[wave] = s;
+  if (lane == 63) wsum[wave] = incl;
+  __syncthreads();
+  int m = incl - n, total = 0;
+  for (int w = 0; w < kRowsThreads / kWave; ++w) {
+    if (w < wave) m += wsum[w];
+    total += wsum[w];
+  }
+  for (int t = t0; t < t1; ++t) {
+    const bool in = counts_of(a, t);
+    a.inv[t] = in ? m : -1;
+    if (in)
+      a.idx[m++] = t;
+    else if (a.token_loss)
+      a.token_loss[t] = 0.f;
+  }
+  for (int i = total + threadIdx.x; i < a.T; i += kRowsThreads) a.idx[i] = 0;   // rows that no result uses
+  if (threadIdx.x == 0) a.counts[0] = total;
+  for (int c = wave; c < a.n_chunks; c += kRowsThreads / kWave)
+    write_plan(a, c, max(0, min(a.chunk, total - c * a.chunk)), lane);
+}
+
+template <typename T>
+__global__ __launch_bounds__(256) void lm_targets_kernel(LmRows a) {
+  const int m = blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (m < a.counts[0]) target_row<T>(a, m, a.idx[m], threadIdx.x & 63);
+}
+
+// sum and maximum over a workgroup of NT threads, in every thread
+template <int NT>
+__device__ __forceinline__ float group_reduce(float v, bool maximum, float* red) {
+#pragma unroll
+  for (int off = 32; off > 0; off >>= 1) {
+    const float o = __shfl_xor(v, off, kWave);
+    v = maximum ? fmaxf(v, o) : v + o;
+  }
+  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
+  __syncthreads();
+  v = red[0];
+#pragma unroll
+  for (int w = 1; w < NT / kWave; ++w) v = maximum ? fmaxf(v, red[w]) : v + red[w];
+  __syncthreads();
+  return v;
+}
+
+// The sums of a row after a piece, by thread 0 of its workgroup; after the last piece its loss.
+__device__ __forceinline__ void row_sums(const LmRows& a, const LmPiece& p, int m, float r0, float r, float s) {
+  const float f0 = r > r0 ? expf(r0 - r) : 1.0f;
+  s = fmaf(a.sum[m], f0, s);
+  a.sum[m] = s;
+  a.alpha[m] = f0;
+  a.ref[m] = r;
+  if (!p.last) return;
+  // s is in units of e^ref
+  const float lt = a.lt[m], own = lt == r ? 1.0f : expf(lt - r);
+  const float nll = lt == r ? log1pf(s) : logf(s + own) + (r - lt);
+  // read by another workgroup of this launch (add_losses): past the XCD's own cache
+  __hip_atomic_store(a.nll + m, nll, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  if (a.token_loss) a.token_loss[a.idx[m]] = nll;
+  a.lse[m] = lt + nll;
+  a.own[m] = -s / (s + own);
+}
+
+__device__ __forceinline__ void add_losses(const LmRows& a) {
+  __shared__ double red[16];
+  const int N = a.counts[0];
+  double s = 0.0;
+  for (int m = threadIdx.x; m < N; m += blockDim.x)
+    s += static_cast<double>(__hip_atomic_load(a.nll + m, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT));
+#pragma unroll
+  for (int off = 32; off > 0; off >>= 1) s += __shfl_xor(s, off, kWave);
+  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = s;
   __syncthreads();
   if (threadIdx.x == 0) {
-    const float f0 = r > r0 ? expf(r0 - r) : 1.0f;
-    a.sum[m] = fmaf(a.sum[m], f0, (red[0] + red[1]) + (red[2] + red[3]));
-    a.alpha[m] = f0;
-    a.ref[m] = r;
+    for (int w = 1; w < static_cast<int>(blockDim.x) / kWave; ++w) s += red[w];
+    a.loss[0] = static_cast<float>(a.scale * (a.mean ? s / max(N, 1) : s));
   }
 }
 
-// log(1 + S) from S = sum e^(lt - ref) ...: the row's sum is in units of its reference
-__device__ __forceinline__ float row_nll(float lt, float ref, float s) {
-  return lt == ref ? log1pf(s) : logf(s + expf(lt - ref)) + (ref - lt);
+// Few tokens: the workgroup whose row is the last to finish adds the losses, in row order, which saves a launch
+// (5 us of 36 where one token is scored).  Without rows the first workgroup writes the loss of none.  Only the
+// rows' losses pass between workgroups, by device-scope stores that are waited for before the count: a
+// device-scope fence instead writes every dirty line of the XCD's cache back (1000 rows 55 us, so 20).
+__device__ __forceinline__ void row_done(const LmRows& a, const LmPiece& p) {
+  __shared__ bool last;
+  if (a.T > kLmSmall || !p.last) return;
+  if (threadIdx.x == 0) {
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    last = __hip_atomic_fetch_add(a.done, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) + 1 ==
+           static_cast<unsigned>(a.counts[0]);
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  }
+  __syncthreads();
+  if (last) add_losses(a);
+}
+__device__ __forceinline__ bool no_row(const LmRows& a, const LmPiece& p, int i) {
+  if (i < *p.count) return false;
+  if (i == 0 && p.last && a.T <= kLmSmall && threadIdx.x == 0) a.loss[0] = 0.f;
+  return true;
 }
 
-// A token a wave, for the tokens whose row is in the chunk; workgroup 0 of the last chunk adds the loss.
-template <typename T>
-__global__ __launch_bounds__(256) void lm_finish_kernel(LmRows a, LmFinish f) {
-  const int lane = threadIdx.x & 63, N = a.counts[0];
-  if (blockIdx.x == 0) {
-    if (!f.last) return;
-    __shared__ double red[256];
-    double s = 0.0;
-    for (int m = threadIdx.x; m < N; m += 256) s += static_cast<double>(row_nll(a.lt[m], a.ref[m], a.sum[m]));
-    red[threadIdx.x] = s;
-    __syncthreads();
-    for (int k = 128; k > 0; k >>= 1) {
-      if (static_cast<int>(threadIdx.x) < k) red[threadIdx.x] += red[threadIdx.x + k];
-      __syncthreads();
+__global__ __launch_bounds__(1024) void lm_sum_kernel(LmRows a) { add_losses(a); }
+
+// The sums of a row's pieces of 64 columns, a workgroup a row.  A piece whose reference is not the row's (a logit
+// far above the target's) raises the row's: then the earlier sums, and this piece's e, are rescaled.
+__global__ __launch_bounds__(256) void lm_combine_kernel(LmRows a, LmPiece p, int parts) {
+  __shared__ float red[4];
+  const int i = blockIdx.x, m = p.m0 + i;
+  if (no_row(a, p, i)) return;
+  const float r0 = a.ref[m];
+  const float2* part = p.part + static_cast<size_t>(i) * parts;
+  float r = r0;
+  float s = 0.f;
+  for (int q = threadIdx.x; q < parts; q += 256) {
+    const float2 v = part[q];
+    r = fmaxf(r, v.x);
+    s += v.y;
+  }
+  r = group_reduce<256>(r, true, red);
+  const bool raised = r > r0;
+  if (raised) {
+    s = 0.f;
+    for (int q = threadIdx.x; q < parts; q += 256) s += part[q].y * expf(part[q].x - r);
+  }
+  s = group_reduce<256>(s, false, red);
+  if (threadIdx.x == 0) row_sums(a, p, m, r0, r, s);
+  if (raised && p.e) {
+    bf16_t* e = static_cast<bf16_t*>(p.e) + static_cast<size_t>(i) * p.pitch;
+    const size_t term = a.mode == kLmSplit ? static_cast<size_t>(p.rows_max) * p.pitch : 0;
+    for (int n = threadIdx.x; n < p.pitch; n += 256) {   // the columns of wave (n & 127) / 32 of tile n / 256
+      // in two halves: e may be e^60 and the factor below the smallest number
+      const float f = expf(0.5f * (part[(n >> 8) * 4 + ((n & 127) >> 5)].x - r));
+      if (term == 0) {
+        e[n] = f32_to_bf16(bf16_to_f32(e[n]) * f * f);
+      } else {
+        float v = (bf16_to_f32(e[n]) + bf16_to_f32(e[n + term]) + bf16_to_f32(e[n + 2 * term])) * f * f;
+        for (int t = 0; t < 3; ++t) {
+          e[n + t * term] = f32_to_bf16(v);
+          v -= bf16_to_f32(e[n + t * term]);
+        }
+      }
     }
-    if (threadIdx.x == 0) f.loss[0] = static_cast<float>(f.scale * (f.mean ? red[0] / max(N, 1) : red[0]));
-    return;
   }
-  const int t = (blockIdx.x - 1) * 4 + (threadIdx.x >> 6);
-  if (t >= a.T) return;
+  row_done(a, p);
+}
+
+// The logits of a piece, in K slices, to e: a workgroup a row; zeros up to the pitch.  MODE kLmF32: in place.
+template <int MODE, int NT>
+__global__ __launch_bounds__(NT) void lm_exp_kernel(LmRows a, LmPiece p) {
+  __shared__ float red[16];
+  const int i = blockIdx.x, m = p.m0 + i;
+  if (no_row(a, p, i)) return;
+  const float r0 = a.ref[m];
+  const int tgt = a.tgt[m] - p.v0;
+  float* l = p.logits + static_cast<size_t>(i) * p.ldl;
+  const size_t slice = static_cast<size_t>(p.rows_max) * p.ldl;
+  float top = r0;
+  for (int n = threadIdx.x; n < p.cols; n += NT) {
+    float v = l[n];
+    for (int z = 1; z < p.slices; ++z) v += l[n + z * slice];
+    if (p.slices > 1) l[n] = v;
+    top = fmaxf(top, v);
+  }
+  top = group_reduce<NT>(top, true, red);
+  // the target's logit is a good reference unless the row rises far above it
+  const float r = top - r0 > 60.0f ? top : r0;
+  const size_t at = static_cast<size_t>(i) * p.pitch, term = static_cast<size_t>(p.rows_max) * p.pitch;
+  float s = 0.f;
+  for (int n = threadIdx.x; n < p.pitch; n += NT) {
+    float v = n < p.cols && n != tgt ? expf(l[n] - r) : 0.f;
+    s += v;
+    if (!p.e) continue;
+    if constexpr (MODE == kLmF32) {
+      static_cast<float*>(p.e)[at + n] = v;
+    } else {
+      bf16_t* e = static_cast<bf16_t*>(p.e) + at + n;
+      for (int t = 0; t < (MODE == kLmSplit ? 3 : 1); ++t) {
+        const bf16_t b = f32_to_bf16(v);
+        e[t * term] = b;
+        v -= bf16_to_f32(b);
+      }
+    }
+  }
+  s = group_reduce<NT>(s, false, red);
+  if (threadIdx.x == 0) row_sums(a, p, m, r0, r, s);
+  row_done(a, p);
+}
+
+// dx of a token: 2048 columns a workgroup, eight a thread, the K slices added in order
+template <typename T>
+__global__ __launch_bounds__(256) void lm_finish_kernel(LmRows a, LmPiece p, int last_chunk, T* __restrict__ dx) {
+  const int t = blockIdx.x, c = 8 * (blockIdx.y * blockDim.x + threadIdx.x);
+  if (c >= a.d) return;
   const int m = a.inv[t];
+  T* out = dx + static_cast<size_t>(t) * a.d + c;
   if (m < 0) {
-    if (!f.last) return;
-    if (lane == 0 && f.token_loss) f.token_loss[t] = 0.f;
-    if (f.dx) {
-      const float z[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-      for (int c = lane; c < a.d / 8; c += kWave) st8(static_cast<T*>(f.dx) + static_cast<size_t>(t) * a.d + 8 * c, z);
-    }
+    const float zero[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    if (last_chunk) st8(out, zero);
     return;
   }
-  if (m < f.m0 || m >= f.m0 + f.chunk) return;
-  const float lt = a.lt[m], ref = a.ref[m], s = a.sum[m], z = s + (lt == ref ? 1.0f : expf(lt - ref));
-  const float unit = f.mean ? f.scale / static_cast<float>(N) : f.scale;
-  if (lane == 0) {
-    const float nll = row_nll(lt, ref, s);
-    if (f.token_loss) f.token_loss[t] = nll;
-    if (f.lse) {
-      f.lse[m] = lt + nll;
-      f.own[m] = -s / z;
-    }
-  }
-  if (!f.dx) return;
-  const T* w = static_cast<const T*>(a.w) + static_cast<size_t>(a.tgt[m]) * a.d;
-  const float* acc = f.acc + static_cast<size_t>(m - f.m0) * a.d;
-  const size_t stride = static_cast<size_t>(f.chunk) * a.d;
-  const float inv = 1.0f / z;
-  for (int c = lane; c < a.d / 8; c += kWave) {
-    float o[8];
-    Raw8<T> wv;
-    wv.load(w + 8 * c);
+  if (m < p.m0 || m >= p.m0 + p.rows_max) return;
+  const int S = a.plan[p.chunk] >> 16;
+  const size_t stride = static_cast<size_t>(*p.count) * a.d;
+  const float* acc = p.acc + static_cast<size_t>(m - p.m0) * a.d + c;
+  Raw8<T> w;
+  w.load(static_cast<const T*>(a.w) + static_cast<size_t>(a.tgt[m]) * a.d + c);
+  float o[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+  for (int z = 0; z < S; ++z) {
     Raw8<float> v;
-    v.load(acc + 8 * c);
+    v.load(acc + z * stride);
 #pragma unroll
-    for (int k = 0; k < 8; ++k) o[k] = v[k];
-    for (int q = 1; q < f.slices; ++q) {
-      v.load(acc + q * stride + 8 * c);
+    for (int k = 0; k < 8; ++k) o[k] += v[k];
+  }
+  const float lt = a.lt[m], ref = a.ref[m], s = a.sum[m], inv = 1.0f / (s + (lt == ref ? 1.0f : expf(lt - ref)));
+  const float unit = a.mean ? a.scale / static_cast<float>(a.counts[0]) : a.scale;
 #pragma unroll
-      for (int k = 0; k < 8; ++k) o[k] += v[k];
+  for (int k = 0; k < 8; ++k) o[k] = unit * ((o[k] - s * w[k]) * inv);
+  st8(out, o);
+}
+
+// ---------------------------------------------------------------------------
+// transposes through 64 x 64 tiles, eight elements a thread on both sides
+// ---------------------------------------------------------------------------
+
+// eight values of a row: bf16, fp32, or three bf16 terms
+template <int MODE>
+__device__ __forceinline__ void put8(void* base, size_t at, size_t term, const float* v) {
+  if constexpr (MODE == kLmF32) {
+    st8(static_cast<float*>(base) + at, v);
+  } else {
+    float r[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) r[k] = v[k];
+    for (int t = 0; t < (MODE == kLmSplit ? 3 : 1); ++t) {
+      st8(static_cast<bf16_t*>(base) + at + t * term, r);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) r[k] -= bf16_to_f32(f32_to_bf16(r[k]));
     }
-#pragma unroll
-    for (int k = 0; k < 8; ++k) o[k] = unit * ((o[k] - s * wv[k]) * inv);
-    st8(static_cast<T*>(f.dx) + static_cast<size_t>(t) * a.d + 8 * c, o);
   }
 }
 
-// xT[i][m] = x[idx[m]][i], zero for m at or past the counted rows; 64 x 64 tiles
-template <typename T>
-__global__ __launch_bounds__(256) void lm_xT_kernel(LmRows a, T* __restrict__ xT, int pitch) {
-  __shared__ T tile[64][65];
-  const int N = a.counts[0], i0 = blockIdx.x * 64, m0 = blockIdx.y * 64;
-  const int tx = threadIdx.x & 63, ty = threadIdx.x >> 6;
-  for (int k = ty; k < 64; k += 4) {
-    const int m = m0 + k;
-    tile[k][tx] = m < N ? static_cast<const T*>(a.x)[static_cast<size_t>(a.idx[m]) * a.d + i0 + tx] : T(0);
-  }
-  __syncthreads();
-  for (int k = ty; k < 64; k += 4) xT[static_cast<size_t>(i0 + k) * pitch + m0 + tx] = tile[tx][k];
-}
+__device__ __forceinline__ int depth_of(int rows) { return max(128, (rows + 63) / 64 * 64); }
 
-// fp32: g[v][m] = unit (p - [target]) from the logits [rows][ldl], transposed
-__global__ __launch_bounds__(256) void lm_g_f32_kernel(LmRows a, int v0, int cols, const float* __restrict__ lse,
-                                                       const float* __restrict__ own, const float* __restrict__ logits,
-                                                       int ldl, float scale, int mean, float* __restrict__ g,
-                                                       int pitch) {
+// in(r, c, v): the eight values of row r at columns c .. c + 7; out(c, r, v): those of column c at rows r ..
+template <class In, class Out>
+__device__ __forceinline__ void transpose64(In in, Out out) {
   __shared__ float tile[64][65];
-  const int N = a.counts[0], n0 = blockIdx.x * 64, m0 = blockIdx.y * 64;
-  const int tx = threadIdx.x & 63, ty = threadIdx.x >> 6;
-  const float unit = mean ? scale / static_cast<float>(max(N, 1)) : scale;
-  for (int k = ty; k < 64; k += 4) {
-    const int m = m0 + k, n = n0 + tx;
-    float v = 0.f;
-    if (m < N && n < cols)
-      v = unit * (a.tgt[m] == v0 + n ? own[m] : expf(logits[static_cast<size_t>(m) * ldl + n] - lse[m]));
-    tile[k][tx] = v;
+#pragma unroll
+  for (int q = threadIdx.x; q < 512; q += 256) {
+    float v[8];
+    in(q >> 3, 8 * (q & 7), v);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) tile[q >> 3][8 * (q & 7) + k] = v[k];
   }
   __syncthreads();
-  for (int k = ty; k < 64; k += 4)
-    if (n0 + k < cols) g[static_cast<size_t>(n0 + k) * pitch + m0 + tx] = tile[tx][k];
+#pragma unroll
+  for (int q = threadIdx.x; q < 512; q += 256) {
+    float v[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) v[k] = tile[8 * (q & 7) + k][q >> 3];
+    out(q >> 3, 8 * (q & 7), v);
+  }
+}
+
+// xT[i][m] = x[idx[m]][i], zero behind the counted rows as far as the dW product reads
+template <int MODE>
+__global__ __launch_bounds__(256) void lm_xT_kernel(LmRows a, void* __restrict__ xT, int pitch) {
+  typedef std::conditional_t<MODE == kLmBf16, bf16_t, float> T;
+  const int N = a.counts[0], i0 = blockIdx.x * 64, m0 = blockIdx.y * 64;
+  if (MODE != kLmF32 && m0 >= depth_of(N)) return;
+  transpose64(
+      [&](int r, int c, float* v) {
+        if (m0 + r < N) {
+          ld8(static_cast<const T*>(a.x) + static_cast<size_t>(a.idx[m0 + r]) * a.d + i0 + c, v);
+        } else {
+          for (int k = 0; k < 8; ++k) v[k] = 0.f;
+        }
+      },
+      [&](int c, int r, const float* v) {
+        put8<MODE>(xT, static_cast<size_t>(i0 + c) * pitch + m0 + r, static_cast<size_t>(a.d) * pitch, v);
+      });
+}
+
+// g[n][m] = p - [n = target]: from e of the whole vocabulary (OF_E), or from fp32 logits; kLmF32: times the unit.
+// A bf16 e is divided by its row's sum and rounded a second time, which saves forming the logits again (1777
+// tokens of d = 1024, vocabulary 50257: 196 us); the target's entry is exact but for its own rounding.
+template <int MODE, bool OF_E>
+__global__ __launch_bounds__(256) void lm_g_kernel(LmRows a, int v0, int cols, const void* __restrict__ src, int ld,
+                                                   size_t src_term, void* __restrict__ g, int pitch) {
+  __shared__ float row[2][64];
+  __shared__ int tgt[64];
+  const int N = a.counts[0], n0 = blockIdx.x * 64, m0 = blockIdx.y * 64;
+  if (MODE != kLmF32 && m0 >= depth_of(N)) return;
+  const float unit = MODE != kLmF32 ? 1.0f : a.mean ? a.scale / static_cast<float>(max(N, 1)) : a.scale;
+  if (threadIdx.x < 64) {
+    const int m = m0 + threadIdx.x;
+    const bool in = m < N;
+    const float lt = in ? a.lt[m] : 0.f, ref = in ? a.ref[m] : 0.f;
+    row[0][threadIdx.x] = !in ? 0.f : OF_E ? unit / (a.sum[m] + (lt == ref ? 1.0f : expf(lt - ref))) : a.lse[m];
+    row[1][threadIdx.x] = in ? unit * a.own[m] : 0.f;
+    tgt[threadIdx.x] = in ? a.tgt[m] - v0 : INT_MIN;
+  }
+  __syncthreads();
+  transpose64(
+      [&](int r, int c, float* v) {
+        if (m0 + r >= N || n0 + c >= ld) {
+          for (int k = 0; k < 8; ++k) v[k] = 0.f;
+          return;
+        }
+        const size_t at = static_cast<size_t>(m0 + r) * ld + n0 + c;
+        const float f = row[0][r];
+        if constexpr (MODE == kLmF32) {
+          ld8(static_cast<const float*>(src) + at, v);
+        } else {
+          ld8(static_cast<const bf16_t*>(src) + at, v);
+          if constexpr (MODE == kLmSplit)
+            for (int t = 1; t < 3; ++t) {
+              float w[8];
+              ld8(static_cast<const bf16_t*>(src) + at + t * src_term, w);
+#pragma unroll
+              for (int k = 0; k < 8; ++k) v[k] += w[k];
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+          v[k] = OF_E ? v[k] * f : unit * expf(v[k] - f);
+          if (n0 + c + k == tgt[r]) v[k] = row[1][r];
+        }
+      },
+      [&](int c, int r, const float* v) {
+        if (n0 + c < cols)
+          put8<MODE>(g, static_cast<size_t>(n0 + c) * pitch + m0 + r, static_cast<size_t>(cols) * pitch, v);
+      });
+}
+
+// w_t[i][v] = w[v][i], zero from the vocabulary to the pitch (a multiple of 64)
+template <typename T>
+__global__ __launch_bounds__(256) void lm_head_kernel(const T* __restrict__ w, int vocab, int d, T* __restrict__ w_t,
+                                                      int pitch) {
+  const int i0 = blockIdx.x * 64, v0 = blockIdx.y * 64;
+  transpose64(
+      [&](int r, int c, float* v) {
+        if (v0 + r < vocab) {
+          ld8(w + static_cast<size_t>(v0 + r) * d + i0 + c, v);
+        } else {
+          for (int k = 0; k < 8; ++k) v[k] = 0.f;
+        }
+      },
+      [&](int c, int r, const float* v) { st8(w_t + static_cast<size_t>(i0 + c) * pitch + v0 + r, v); });
+}
+
+__global__ __launch_bounds__(256) void lm_terms_kernel(const float* __restrict__ in, int ld_in, const int* __restrict__ idx,
+                                                       const int* __restrict__ count, int cols, size_t term,
+                                                       bf16_t* __restrict__ out) {
+  const int r = blockIdx.x, c = 8 * (blockIdx.y * 256 + threadIdx.x);
+  if ((count && r >= *count) || c >= cols) return;
+  float v[8];
+  ld8(in + static_cast<size_t>(idx ? idx[r] : r) * ld_in + c, v);
+  put8<kLmSplit>(out, static_cast<size_t>(r) * cols + c, term, v);
+}
+
+// a row of few columns takes few threads, so that more rows are under way
+template <int MODE>
+void lm_exp(const LmRows& a, const LmPiece& p, hipStream_t s) {
+  if (p.pitch <= 2048)
+    lm_exp_kernel<MODE, 256><<<p.rows_max, 256, 0, s>>>(a, p);
+  else
+    lm_exp_kernel<MODE, 1024><<<p.rows_max, 1024, 0, s>>>(a, p);
 }
 
 }  // namespace
 
-hipError_t launch_lm_rows(const LmRows& a, int chunk, int n_chunks, hipStream_t s) {
-  lm_rows_kernel<<<1, kRowsThreads, 0, s>>>(a, chunk, n_chunks);
-  return hipGetLastError();
-}
-
-hipError_t launch_lm_targets(const LmRows& a, hipStream_t s) {
-  if (a.dtype == 1)
+hipError_t launch_lm_rows(const LmRows& a, hipStream_t s) {
+  const bool b16 = a.mode == kLmBf16;
+  if (a.T <= kLmSmall) {
+    if (b16)
+      lm_rows_small_kernel<bf16_t><<<(a.T + 3) / 4, 256, 0, s>>>(a);
+    else
+      lm_rows_small_kernel<float><<<(a.T + 3) / 4, 256, 0, s>>>(a);
+    return hipGetLastError();
+  }
+  lm_rows_kernel<<<1, kRowsThreads, 0, s>>>(a);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  if (b16)
     lm_targets_kernel<bf16_t><<<(a.T + 3) / 4, 256, 0, s>>>(a);
   else
     lm_targets_kernel<float><<<(a.T + 3) / 4, 256, 0, s>>>(a);
   return hipGetLastError();
 }
 
-hipError_t launch_lm_combine(const LmRows& a, const LmPiece& p, hipStream_t s) {
-  if (a.dtype == 1)
-    lm_combine_kernel<<<(p.rows_max + 3) / 4, 256, 0, s>>>(a, p, lm_parts(p.cols));
-  else
-    lm_exp_f32_kernel<<<p.rows_max, 256, 0, s>>>(a, p);
+hipError_t launch_lm_sum(const LmRows& a, hipStream_t s) {
+  lm_sum_kernel<<<1, 1024, 0, s>>>(a);
   return hipGetLastError();
 }
 
-hipError_t launch_lm_finish(const LmRows& a, const LmFinish& f, hipStream_t s) {
-  if (a.dtype == 1)
-    lm_finish_kernel<bf16_t><<<1 + (a.T + 3) / 4, 256, 0, s>>>(a, f);
+hipError_t launch_lm_combine(const LmRows& a, const LmPiece& p, hipStream_t s) {
+  if (!p.logits)
+    lm_combine_kernel<<<p.rows_max, 256, 0, s>>>(a, p, lm_parts(p.cols));
+  else if (a.mode == kLmBf16)
+    lm_exp<kLmBf16>(a, p, s);
+  else if (a.mode == kLmF32)
+    lm_exp<kLmF32>(a, p, s);
   else
-    lm_finish_kernel<float><<<1 + (a.T + 3) / 4, 256, 0, s>>>(a, f);
+    lm_exp<kLmSplit>(a, p, s);
+  return hipGetLastError();
+}
+
+hipError_t launch_lm_finish(const LmRows& a, const LmPiece& p, void* dx, hipStream_t s) {
+  const int nt = std::min(256, (a.d / 8 + 63) / 64 * 64);
+  const dim3 grid(a.T, (a.d / 8 + nt - 1) / nt);
+  const int last = p.chunk == a.n_chunks - 1;
+  if (a.mode == kLmBf16)
+    lm_finish_kernel<bf16_t><<<grid, nt, 0, s>>>(a, p, last, static_cast<bf16_t*>(dx));
+  else
+    lm_finish_kernel<float><<<grid, nt, 0, s>>>(a, p, last, static_cast<float*>(dx));
   return hipGetLastError();
 }
 
 hipError_t launch_lm_xT(const LmRows& a, void* xT, int pitch, hipStream_t s) {
   const dim3 grid(a.d / 64, pitch / 64);
-  if (a.dtype == 1)
-    lm_xT_kernel<bf16_t><<<grid, 256, 0, s>>>(a, static_cast<bf16_t*>(xT), pitch);
+  if (a.mode == kLmBf16)
+    lm_xT_kernel<kLmBf16><<<grid, 256, 0, s>>>(a, xT, pitch);
+  else if (a.mode == kLmF32)
+    lm_xT_kernel<kLmF32><<<grid, 256, 0, s>>>(a, xT, pitch);
   else
-    lm_xT_kernel<float><<<grid, 256, 0, s>>>(a, static_cast<float*>(xT), pitch);
+    lm_xT_kernel<kLmSplit><<<grid, 256, 0, s>>>(a, xT, pitch);
   return hipGetLastError();
 }
 
-hipError_t launch_lm_g_f32(const LmRows& a, int v0, int cols, const float* lse, const float* own, const float* logits,
-                           int ldl, float scale, bool mean, float* g, int pitch, hipStream_t s) {
-  lm_g_f32_kernel<<<dim3((cols + 63) / 64, pitch / 64), 256, 0, s>>>(a, v0, cols, lse, own, logits, ldl, scale,
-                                                                     mean ? 1 : 0, g, pitch);
+hipError_t launch_lm_g(const LmRows& a, int v0, int cols, const void* ws, const float* logits, int ldl, void* g, int pitch,
+                       hipStream_t s) {
+  if (a.mode != kLmF32) return launch_lm_g_products(a, v0, cols, ws, g, pitch, s);
+  lm_g_kernel<kLmF32, false><<<dim3((cols + 63) / 64, pitch / 64), 256, 0, s>>>(a, v0, cols, logits, ldl, 0, g, pitch);
+  return hipGetLastError();
+}
+
+hipError_t launch_lm_g_of_e(const LmRows& a, const LmPiece& p, void* g, int pitch, hipStream_t s) {
+  const dim3 grid((p.cols + 63) / 64, pitch / 64);
+  const size_t term = static_cast<size_t>(p.rows_max) * p.pitch;
+  if (a.mode == kLmBf16)
+    lm_g_kernel<kLmBf16, true><<<grid, 256, 0, s>>>(a, 0, p.cols, p.e, p.pitch, term, g, pitch);
+  else if (a.mode == kLmF32)
+    lm_g_kernel<kLmF32, true><<<grid, 256, 0, s>>>(a, 0, p.cols, p.e, p.pitch, term, g, pitch);
+  else
+    lm_g_kernel<kLmSplit, true><<<grid, 256, 0, s>>>(a, 0, p.cols, p.e, p.pitch, term, g, pitch);
+  return hipGetLastError();
+}
+
+hipError_t launch_lm_terms(const float* in, int ld_in, const int* idx, const int* count, int rows, int cols, void* out,
+                           hipStream_t s) {
+  lm_terms_kernel<<<dim3(rows, (cols + 2047) / 2048), 256, 0, s>>>(in, ld_in, idx, count, cols,
+                                                                   static_cast<size_t>(rows) * cols, static_cast<bf16_t*>(out));
+  return hipGetLastError();
+}
+
+hipError_t launch_lm_head(int dtype, const void* w, int vocab, int d, void* w_t, int pitch, hipStream_t s) {
+  const dim3 grid(d / 64, pitch / 64);
+  if (dtype == 1)
+    lm_head_kernel<bf16_t><<<grid, 256, 0, s>>>(static_cast<const bf16_t*>(w), vocab, d, static_cast<bf16_t*>(w_t), pitch);
+  else
+    lm_head_kernel<float><<<grid, 256, 0, s>>>(static_cast<const float*>(w), vocab, d, static_cast<float*>(w_t), pitch);
   return hipGetLastError();
 }
 

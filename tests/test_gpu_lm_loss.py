@@ -32,7 +32,8 @@ def _check(c, y):
 
 
 SIZES = [(1, 256, 65), (1, 512, 2003), (2, 256, 127), (3, 256, 128), (17, 512, 256), (63, 256, 257), (64, 768, 320),
-         (65, 256, 1000), (129, 512, 4001), (257, 256, 2003), (300, 1024, 511), (600, 256, 3001), (1025, 256, 1537)]
+         (65, 256, 1000), (129, 512, 4001), (257, 256, 2003), (300, 1024, 511), (600, 256, 3001), (1025, 256, 1537),
+         (1, 256, 40001), (5, 256, 33000), (300, 256, 20011), (130, 1280, 700), (2000, 256, 8000)]
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
@@ -57,12 +58,23 @@ def test_outputs_are_optional(dx, dw, dtype):
         assert torch.equal(c.out[k].t, full.out[k].t), k
 
 
-@pytest.mark.parametrize("T,V,dtype", [(8192 + 9, 16384 + 300, "bf16"), (8192 + 9, 8192 + 200, "f32"), (8192, 32768 + 77, "bf16")])
-def test_chunks_of_rows_and_pieces_of_the_vocabulary(T, V, dtype):
+@pytest.mark.parametrize("d,V", [(384, 64), (384, 1000), (128, 5000)])
+@pytest.mark.parametrize("T", [1, 40, 400])
+def test_fp32_widths_of_half_a_tile(T, d, V):
+    """d a multiple of 128 only, vocabularies below 65: fp32 models alone."""
     from tests import train_ends as E
-    print(f"case lm_loss pieces T={T} V={V} {dtype}", flush=True)
-    x, w, y = _inputs(T, 256, V, dtype, 1, keep=0.97)
-    _check(E.Loss(x, w, y, dw=dtype == "bf16").run(), y)
+    print(f"case lm_loss f32 T={T} d={d} V={V}", flush=True)
+    x, w, y = _inputs(T, d, V, "f32", T + d, keep=1.0 if T < 4 else 0.7)
+    _check(E.Loss(x, w, y).run(), y)
+
+
+@pytest.mark.parametrize("T,d,V,dtype", [(8192 + 9, 256, 16384 + 300, "bf16"), (8192 + 9, 256, 5376 + 200, "f32"),
+                                         (8192, 256, 32768 + 77, "bf16"), (2000, 384, 33800, "f32"), (1500, 256, 30000, "f32")])
+def test_chunks_of_rows_and_pieces_of_the_vocabulary(T, d, V, dtype):
+    from tests import train_ends as E
+    print(f"case lm_loss pieces T={T} d={d} V={V} {dtype}", flush=True)
+    x, w, y = _inputs(T, d, V, dtype, 1, keep=0.97)
+    _check(E.Loss(x, w, y).run(), y)
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
@@ -75,19 +87,20 @@ def test_logits_far_above_the_target(T, size, dtype):
     _check(E.Loss(x, w, y, mean=False).run(), y)
 
 
-def test_reference_moves_between_pieces():
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_reference_moves_between_pieces(dtype):
     """The target in the first piece, a logit 200 above it in the last, another 150 above it before."""
     import torch
     from tests import train_ends as E
     T, d, V = 8192, 256, 40000
-    print("case lm_loss far, by pieces", flush=True)
+    print(f"case lm_loss far, by pieces {dtype}", flush=True)
     g = torch.Generator().manual_seed(3)
     w = torch.randn(V, d, generator=g) * 0.02
     x = torch.randn(T, d, generator=g)
     w[20000] = x[5] / x[5].norm() * 9.5
     w[39999] = x[5] / x[5].norm() * 13.0
     w[30000] = -x[7] / x[7].norm() * 14.0
-    x, w = x.to(E.DEV).bfloat16(), w.to(E.DEV).bfloat16()
+    x, w = x.to(E.DEV).to(E.TORCH[dtype]), w.to(E.DEV).to(E.TORCH[dtype])
     y = np.full(T, -1)
     y[[0, 5, 7, 4000, 8191]] = [9, 100, 30000, 39999, 20000]
     _check(E.Loss(x, w, y, dw=False).run(), y)
@@ -214,7 +227,7 @@ def test_two_calls_on_two_streams():
     import torch
     from tests import train_ends as E
     print("case lm_loss two streams", flush=True)
-    a, b = _inputs(500, 512, 3000, "bf16", 21), _inputs(333, 512, 2500, "bf16", 22)
+    a, b = _inputs(500, 512, 3000, "bf16", 21), _inputs(333, 512, 2500, "f32", 22)
     ca, cb = E.Loss(*a), E.Loss(*b)
     sa, sb = torch.cuda.Stream(), torch.cuda.Stream()
     torch.cuda.synchronize()
@@ -227,7 +240,7 @@ def test_two_calls_on_two_streams():
     _check(cb, b[2])
 
 
-@pytest.mark.parametrize("T,dtype", [(5, "bf16"), (300, "bf16"), (70, "f32")])
+@pytest.mark.parametrize("T,dtype", [(5, "bf16"), (300, "bf16"), (70, "f32"), (1200, "f32"), (1100, "bf16")])
 def test_graph_replays_with_new_inputs(T, dtype):
     """Targets, and with them the number of rows, change between the replays; eager work runs in between."""
     import torch

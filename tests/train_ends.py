@@ -80,14 +80,18 @@ def loss_bounds(x, w, y, scale, mean, dtype):
     """Bounds of |result - 64 bits| by the roundings on the way, from the same inputs in 64 bits.
 
     u: half a step of the stored exponentials and outputs; g = n 2^-24: n fp32 additions in any order.
-      logit      d 2^-24 sum |x W|, of the column and of the target: a relative error of e = exp(l - ref)
+      logit      d 2^-24 sum |x W|, of the column and of the target: a relative error of e = exp(l - ref); fp32 products
+                 may be six bf16 products of three-term operands, six additions each (a: 6), that leave out 3 2^-24
       exp        a step or two, and the rounding of its argument: 2^-22 (|l - ref| + 4)
       S          the sum's order: at most V / 64 + 64 additions one after another
-      dx, dW     e (or p) stored in u, twice where a reference moved (a logit 60 above the target's), V or N additions
+      dx         e stored in u, twice where a reference moved (a logit 60 above the target's); V additions
+      dW         p stored in u, or e divided by its row's sum and stored a second time, and where a reference moved a
+                 third; the target's p - 1 once; N additions
       below 2^-126 an exponential may be zero: e is at least one somewhere in each row's sum, so p loses at most 2^-126 a
                  column, dx 2^-126 sum |W| and dW 2^-126 sum |x| (times the unit), and a result itself at most 2^-126
     """
     u, s24, tiny = HALF_STEP[dtype], 2.0 ** -24, 2.0 ** -126
+    a = 6 if dtype == "f32" else 1
     T, d = x.shape
     V = w.shape[0]
     rows = np.flatnonzero((y >= 0) & (y < V))
@@ -106,17 +110,17 @@ def loss_bounds(x, w, y, scale, mean, dtype):
     z = p.sum(axis=1)
     p /= z[:, None]
     rest = 1.0 - p[at]
-    eps = 2 * d * s24 * size + 4 * s24 * (np.max(np.abs(l - ref[:, None]), axis=1) + 4)
+    eps = 2 * (a * d + 3) * s24 * size + 4 * s24 * (np.max(np.abs(l - ref[:, None]), axis=1) + 4)
     eps = np.expm1(eps) + (V / 64 + 64) * s24
     p[at] = 0.0
     nll = np.log(z) + top - lt
     tok[rows] = np.minimum(1.0, p.sum(axis=1) * 1.001 + 1e-30) * eps + 8 * s24 * np.abs(nll) + 2 * d * s24 * size * rest
     ue = u * np.where(top - lt > 59.0, 2.01, 1.01)
-    dx[rows] = unit * (((ue + eps + V * s24)[:, None] * p) @ np.abs(w) + (rest * (eps + 8 * s24))[:, None] * np.abs(w[y[rows]]))
+    dx[rows] = unit * (((ue + eps + (a * V + 3) * s24)[:, None] * p) @ np.abs(w) + (rest * (eps + 8 * s24))[:, None] * np.abs(w[y[rows]]))
     dx[rows] += tiny + unit * tiny * np.abs(w).sum(0)
-    g = p
-    g[at] = rest
-    dw = unit * ((g * (1.01 * u + eps + (n + d) * s24)[:, None]).T @ np.abs(xr)) + tiny + unit * tiny * np.abs(xr).sum(0)
+    g = p * (ue + 1.01 * u + eps + (a * n + 3) * s24)[:, None]
+    g[at] = rest * (1.01 * u + eps + (a * n + 3) * s24)
+    dw = unit * (g.T @ np.abs(xr)) + tiny + unit * tiny * np.abs(xr).sum(0)
     return float(tok.sum() * unit + 2 * s24 * unit * np.abs(nll).sum()), tok, dx, dw
 
 
