@@ -1703,7 +1703,7 @@ bool any_overlap(const Region (&written)[W], const Region (&read)[R]) {
 }
 
 constexpr int kLmChunk = 8192;               // rows of one chunk
-constexpr size_t kLmPieceBytes = 256u << 20; // of e (or of dW's g) for one chunk and piece: the last-level cache's size
+constexpr size_t kLmPiece = 128u << 20;      // elements of e (or of dW's g) of one chunk and piece: 256 MiB in bf16
 constexpr int kLmVocabMax = 65535 * 64;      // grid limit of the head's transpose
 constexpr int kLmVocabMin = 65;              // matrix cores: the products take K in at least two k-tiles
 constexpr int kLmHeadRows = 1 << 17;         // head rows of a product, which addresses them with 32 bits
@@ -1745,8 +1745,8 @@ LmLayout lm_layout_of(const hero_dims& d, int vocab, int T, bool dx, bool dw) {
   const int ktiles = d.d / 64 * (split ? 6 : 1);
   // whole tiles of 256 columns whose e (or g) fits the piece, and whose head rows' terms do
   auto fit = [&](size_t rows) {
-    size_t c = kLmPieceBytes / (es * rows);
-    if (split) c = std::min(c, kLmPieceBytes / (6 * w));
+    size_t c = kLmPiece / rows;
+    if (split) c = std::min(c, kLmPiece / w);
     const size_t most = std::min<size_t>((static_cast<size_t>(vocab) + 255) / 256 * 256, kLmHeadRows - 256);
     return static_cast<int>(std::min(std::max<size_t>(c / 256 * 256, 256), most));
   };
@@ -1787,7 +1787,7 @@ LmLayout lm_layout_of(const hero_dims& d, int vocab, int T, bool dx, bool dw) {
   L.logits = take(L.slices * c * L.ldl * 4);
   L.acc = take(L.acc_rows * w * 4);
   L.xs = take(split ? t * w * 6 : 0);
-  L.g_pitch = std::max(128, up(T, 64));
+  L.g_pitch = mfma ? std::max(128, up(T, 64)) : up(T, 64);
   L.g_cols = L.single ? vocab : fit(static_cast<size_t>(L.g_pitch));
   L.g_ldl = up(std::min(L.g_cols, vocab), 64);
   L.ws = take(split ? std::max<size_t>(widest, dw && !L.single ? std::min(L.g_cols, vocab) : 0) * w * 6 : 0);

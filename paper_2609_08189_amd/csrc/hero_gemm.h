@@ -163,7 +163,7 @@ struct SixTerm<E, std::void_t<decltype(E::kSixTerm)>> : std::true_type {};
 constexpr uint32_t kTermA = 0x120100, kTermB = 0x102010;   // term of the s-th product: bits 4 s
 
 // An epilogue with kColumns prepares what its columns combine with once a tile (Epi::Cols, for the eight
-// columns that a lane emits in every row block); skip(n0) leaves a tile of columns out.
+// columns that a lane emits in every row block).
 template <class E, class = void>
 struct ColumnsHook : std::false_type {
   struct Cols {};
@@ -201,21 +201,13 @@ __device__ __forceinline__ void swiglu_bwd_tile(const Epi& epi, f32x4 (&acc)[2 *
 
 template <class C, class Epi>
 __device__ __forceinline__ void phase_tile(const ARows<bf16_t>& A, const BRows<bf16_t>& B, const Epi& epi, int M,
-                                           int M_max, int K, int n_tiles, unsigned char* smem, int bid, int slice,
+                                           int mt_act, int K, int n_tiles, unsigned char* smem, int tile, int slice,
                                            int slices) {
   constexpr int BM = C::BM, HM = C::HM, HB = C::HB, NW = C::NW, BH = C::BH;
-  const int mt_max = (M_max + BM - 1) / BM;
-  const int mt_act = min(mt_max, (M + BM - 1) / BM);
-  const int per = (mt_act * n_tiles + 7) >> 3;
-  const int q = bid >> 3;
-  if (q >= per) return;
-  const int tile = (bid & 7) * per + q;
-  if (tile >= mt_act * n_tiles) return;
+  if (tile < 0 || tile >= mt_act * n_tiles) return;
   const int grp = tile / (GROUP_M * n_tiles), rem = tile % (GROUP_M * n_tiles);
   const int gsz = min(GROUP_M, mt_act - grp * GROUP_M);
   const int mt = grp * GROUP_M + rem % gsz, nt = rem / gsz;
-  if constexpr (ColumnsHook<Epi>::value)
-    if (epi.skip(nt * C::BN)) return;
   uint32_t turn = A.turn;
   if constexpr (DeviceDepth<Epi>::value) {
     K = epi.depth();
@@ -471,11 +463,22 @@ __device__ __forceinline__ void phase_tile(const ARows<bf16_t>& A, const BRows<b
 }
 
 
+// Row tiles of M rows, at most those the grid was sized for
+__device__ __forceinline__ int row_tiles(int M, int M_max, int BM) {
+  return min((M_max + BM - 1) / BM, (M + BM - 1) / BM);
+}
+// The tile of workgroup b: each XCD (b mod 8) takes a contiguous range of the grouped order; -1: none
+__device__ __forceinline__ int tile_of(int b, int tiles) {
+  const int per = (tiles + 7) >> 3;
+  return (b >> 3) < per ? (b & 7) * per + (b >> 3) : -1;
+}
+
 template <class C, class Epi>
 __global__ __launch_bounds__(512, 2) void phase_gemm(ARows<bf16_t> A, BRows<bf16_t> B, Epi epi,
                                                      const int* __restrict__ m_count, int M_max, int K, int n_tiles) {
   __shared__ __attribute__((aligned(1024))) unsigned char smem[2 * C::STAGE];
-  phase_tile<C>(A, B, epi, m_count ? *m_count : M_max, M_max, K, n_tiles, smem, blockIdx.x, blockIdx.y, gridDim.y);
+  const int M = m_count ? *m_count : M_max, mt = row_tiles(M, M_max, C::BM);
+  phase_tile<C>(A, B, epi, M, mt, K, n_tiles, smem, tile_of(blockIdx.x, mt * n_tiles), blockIdx.y, gridDim.y);
 }
 
 // Tile height for M rows: the launch's time in rounds of workgroups over the CUs, times the
@@ -502,6 +505,18 @@ __host__ __device__ inline int phase_rows(int M, int n_tiles) {
 template <class Epi>
 constexpr bool kSpill = DualHook<Epi>::value || TwoTerm<Epi>::value;
 
+// one of the three tile heights, chosen on the device
+template <bool DUAL, class Epi>
+__device__ __forceinline__ void phase_any(int bm, const ARows<bf16_t>& A, const BRows<bf16_t>& B, const Epi& epi, int M,
+                                          int mt, int K, int n_tiles, unsigned char* smem, int tile, int slice, int slices) {
+  if (bm == 256)
+    phase_tile<Phase<256, DUAL>>(A, B, epi, M, mt, K, n_tiles, smem, tile, slice, slices);
+  else if (bm == 192)
+    phase_tile<Phase<192, DUAL>>(A, B, epi, M, mt, K, n_tiles, smem, tile, slice, slices);
+  else
+    phase_tile<Phase<128, DUAL>>(A, B, epi, M, mt, K, n_tiles, smem, tile, slice, slices);
+}
+
 // Threshold routing: the host only knows an upper bound of the row count, so the workgroups choose
 // the tile height themselves from the count on the device.
 template <bool DUAL, class Epi>
@@ -510,13 +525,8 @@ __global__ __launch_bounds__(512, 2) void phase_gemm_any(ARows<bf16_t> A, BRows<
                                                          int n_tiles) {
   __shared__ __attribute__((aligned(1024))) unsigned char smem[2 * Phase<256, DUAL>::STAGE];
   const int M = min(*m_count, M_max);
-  const int bm = phase_rows<kSpill<Epi>>(M, n_tiles);
-  if (bm == 256)
-    phase_tile<Phase<256, DUAL>>(A, B, epi, M, M_max, K, n_tiles, smem, blockIdx.x, blockIdx.y, gridDim.y);
-  else if (bm == 192)
-    phase_tile<Phase<192, DUAL>>(A, B, epi, M, M_max, K, n_tiles, smem, blockIdx.x, blockIdx.y, gridDim.y);
-  else
-    phase_tile<Phase<128, DUAL>>(A, B, epi, M, M_max, K, n_tiles, smem, blockIdx.x, blockIdx.y, gridDim.y);
+  const int bm = phase_rows<kSpill<Epi>>(M, n_tiles), mt = row_tiles(M, M_max, bm);
+  phase_any<DUAL>(bm, A, B, epi, M, mt, K, n_tiles, smem, tile_of(blockIdx.x, mt * n_tiles), blockIdx.y, gridDim.y);
 }
 
 // exact: M_max is the row count (m_count, if given, holds at most that)

@@ -452,6 +452,7 @@ struct LmPiece {
   const void* wts;           // kLmSplit: [3][d][pitch] ... transposed
   float* acc;                // [slices of the plan][rows][d] sum over the vocabulary of e W
 };
+constexpr int kLmLogitsMax = 8192;   // columns of a piece whose logits are kept (kLmF32: of any)
 int lm_parts(int cols);
 int lm_logit_slices(int rows, int cols, int ktiles);
 hipError_t launch_lm_logits(const LmRows& a, const LmPiece& p, hipStream_t s);

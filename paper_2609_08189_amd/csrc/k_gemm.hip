@@ -2505,8 +2505,13 @@ __global__ __launch_bounds__(256) void lm_f32_dx(ARows<float> A, BRows<float> B,
 
 hipError_t launch_lm_f32_logits(const float* x, const int* idx, const int* count, int rows_max, const float* w, int cols,
                                 int d, float* out, int ldl, hipStream_t s) {
-  return run_f32<false>(ARows<float>{x, idx, d}, BRows<float>{w, nullptr, INT_MAX, d}, EpiStoreF32{out, ldl, 0}, count,
-                        rows_max, cols, d, s);
+  const ARows<float> A{x, idx, d};
+  const BRows<float> B{w, nullptr, INT_MAX, d};
+  const EpiStoreF32 epi{out, ldl, 0};
+  // 64 x 64 tiles read a head row once for up to 64 tokens
+  if (rows_max > 32 && (cols + 63) / 64 * ((rows_max + 63) / 64) >= kCUs)
+    return run_f32_r<false, 4>(A, B, epi, count, rows_max, cols, d, true, s);
+  return run_f32<false>(A, B, epi, count, rows_max, cols, d, s);
 }
 
 // K slices of the dx product: 32 x 32 tiles that leave CUs idle share K, a slice of at least 512
@@ -2519,6 +2524,12 @@ hipError_t launch_lm_f32_dx(const float* e, const int* count, int rows_max, int 
                             int slices, const float* alpha, bool first, float* acc, hipStream_t s) {
   const int Kz = (pitch + slices * 16 - 1) / (slices * 16) * 16;
   const dim3 grid((rows_max + 31) / 32, (d + 31) / 32, slices);
+  if (rows_max > 32) {
+    const dim3 g4((rows_max + 63) / 64, (d + 63) / 64, slices);
+    lm_f32_dx<4><<<g4, 256, 0, s>>>(ARows<float>{e, nullptr, pitch}, BRows<float>{w_t, nullptr, INT_MAX, ld_wt},
+                                    EpiLmF32{acc, d, alpha, first}, count, d, pitch, Kz);
+    return hipGetLastError();
+  }
   lm_f32_dx<2><<<grid, 256, 0, s>>>(ARows<float>{e, nullptr, pitch}, BRows<float>{w_t, nullptr, INT_MAX, ld_wt},
                                     EpiLmF32{acc, d, alpha, first}, count, d, pitch, Kz);
   return hipGetLastError();

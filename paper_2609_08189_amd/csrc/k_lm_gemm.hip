@@ -159,7 +159,6 @@ struct EpiLmG : Six<SIX> {
   };
   struct Pre {};
   __device__ __forceinline__ Pre prep(int, int) const { return {}; }
-  __device__ __forceinline__ bool skip(int n0) const { return n0 >= lm_depth(count); }
   __device__ __forceinline__ Cols cols(int n) const {
     Cols c;
     const int N = *count;
@@ -204,26 +203,41 @@ struct EpiLmDw : Six<SIX> {   // dw[m][n] = unit acc, the tokens as K
   }
 };
 
-// The dx product on the tile height and K slices that the rows' plan names; slice z into acc + z M d.
-// The grid covers any plan: the workgroups of a slice come one after another, a multiple of eight, so
-// that each XCD keeps its share of every slice's tile order.
+// The dx product on the tile height and K slices that the rows' plan names; slice z into acc + z M d.  Workgroups
+// go to the XCDs round-robin: an XCD keeps to one slice (S < 8: 8 / S XCDs share one; S a multiple of 8: S / 8
+// slices one after another), so that what its tiles read, all rows of e and of W^T over the slice's columns,
+// passes through its L2 once.  With every slice spread over all XCDs, 1173 rows of d = 1024 against 50257 columns
+// in 12 slices took 212 us (about 1 GB fetched where the operands are 220 MB).
 template <class Epi>
 __global__ __launch_bounds__(512, 2) void lm_dx_kernel(ARows<bf16_t> A, BRows<bf16_t> B, Epi epi,
                                                        const int* __restrict__ m_count, const int* __restrict__ plan,
                                                        int M_max, int K, int n_tiles) {
   __shared__ __attribute__((aligned(1024))) unsigned char smem[2 * Phase<256, false>::STAGE];
   const int M = min(*m_count, M_max), bm = *plan & 0xffff, S = *plan >> 16;
-  const int per = ((M + bm - 1) / bm * n_tiles + 7) / 8 * 8;
-  if (per == 0) return;
-  const int z = static_cast<int>(blockIdx.x) / per, bid = static_cast<int>(blockIdx.x) % per;
+  const int mt = row_tiles(M, M_max, bm), tiles = mt * n_tiles;
+  if (tiles == 0) return;
+  const int x = static_cast<int>(blockIdx.x) & 7, q = static_cast<int>(blockIdx.x) >> 3;
+  int z, tile;
+  if (S >= 8) {
+    z = x + 8 * (q / tiles);
+    tile = q % tiles;
+  } else {
+    const int g = 8 / S, per = (tiles + g - 1) / g;
+    z = x / g;
+    tile = q < per ? x % g * per + q : -1;
+  }
   if (z >= S) return;
   epi.out += static_cast<size_t>(z) * M * epi.ld;
-  if (bm == 256)
-    phase_tile<Phase<256, false>>(A, B, epi, M, M_max, K, n_tiles, smem, bid, z, S);
-  else if (bm == 192)
-    phase_tile<Phase<192, false>>(A, B, epi, M, M_max, K, n_tiles, smem, bid, z, S);
-  else
-    phase_tile<Phase<128, false>>(A, B, epi, M, M_max, K, n_tiles, smem, bid, z, S);
+  phase_any<false>(bm, A, B, epi, M, mt, K, n_tiles, smem, tile, z, S);
+}
+
+// g's product: as many columns as there are counted tokens, so the tile height is chosen on the device
+template <class Epi>
+__global__ __launch_bounds__(512, 2) void lm_g_product(ARows<bf16_t> A, BRows<bf16_t> B, Epi epi, int M, int K) {
+  __shared__ __attribute__((aligned(1024))) unsigned char smem[2 * Phase<256, false>::STAGE];
+  const int n_tiles = (lm_depth(epi.count) + 255) / 256;
+  const int bm = phase_rows<false>(M, n_tiles), mt = row_tiles(M, M, bm);
+  phase_any<false>(bm, A, B, epi, M, mt, K, n_tiles, smem, tile_of(blockIdx.x, mt * n_tiles), 0, 1);
 }
 
 int lm_tiles(int n) { return (n + 255) / 256; }
@@ -264,7 +278,7 @@ hipError_t lm_dx(const LmRows& a, const LmPiece& p, const void* w_t, int ld_wt, 
   if constexpr (SIX) B = {static_cast<const bf16_t*>(p.wts), nullptr, INT_MAX, p.pitch, INT_MAX, nullptr,
                           static_cast<size_t>(a.d) * p.pitch};
   const int n_tiles = a.d / 256, K = SIX ? 6 * p.pitch : p.pitch;
-  const int blocks = std::max((p.rows_max + 127) / 128 * n_tiles, kLmDxBlocks) + 8 * kLmDxSlices;
+  const int blocks = (std::max((p.rows_max + 127) / 128 * n_tiles, kLmDxBlocks) + 7) / 8 * 8 + 8;
   const float* alpha = a.alpha + p.m0;
   const int* plan = a.plan + p.chunk;
   if (p.first)
@@ -283,7 +297,11 @@ hipError_t lm_g(const LmRows& a, int v0, int cols, const void* ws, void* g, int 
     B = {static_cast<const bf16_t*>(a.xs), nullptr, INT_MAX, a.d, a.T - 1, nullptr, static_cast<size_t>(a.T) * a.d};
   }
   const EpiLmG<SIX> epi{{}, a.lse, a.own, a.tgt, a.counts, v0, pitch, static_cast<bf16_t*>(g), static_cast<size_t>(cols) * pitch};
-  return run_phase<false>(A, B, epi, nullptr, cols, lm_tiles(pitch) * 256, SIX ? 6 * a.d : a.d, s);
+  const auto blocks = [&](int bm) { return ((cols + bm - 1) / bm * lm_tiles(pitch) + 7) / 8 * 8; };
+  // enough for any choice of any count
+  const int grid = std::max({blocks(256), std::min(blocks(192), 8 * kCUs + 8), std::min(blocks(128), 4 * kCUs + 8)});
+  lm_g_product<<<grid, 512, 0, s>>>(A, B, epi, cols, SIX ? 6 * a.d : a.d);
+  return hipGetLastError();
 }
 
 template <typename T, bool SIX>
@@ -303,7 +321,7 @@ int lm_parts(int cols) { return 4 * lm_tiles(cols); }
 // epilogue's exponentials 5)
 int lm_logit_slices(int rows, int cols, int ktiles) {
   const int tiles = (rows + 127) / 128 * lm_tiles(cols);
-  return 2 * tiles > kCUs || cols > 8192 ? 1 : std::max(1, std::min(kCUs / tiles, ktiles / 4));
+  return 2 * tiles > kCUs || cols > kLmLogitsMax - 256 ? 1 : std::max(1, std::min(kCUs / tiles, ktiles / 4));
 }
 
 hipError_t launch_lm_logits(const LmRows& a, const LmPiece& p, hipStream_t s) {
