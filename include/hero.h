@@ -679,7 +679,8 @@ typedef struct hero_lm_loss_out {
 } hero_lm_loss_out;
 
 /* Workspace bytes for hero_lm_loss with and without the two gradients (nonzero: wanted).  Host-only.  About
- * 0.3 GiB, with dx 4 d bytes more per token (at most 8192 of them), with dw 2 d per token. */
+ * 0.5 GiB for the exponentials of a piece and, with dx, 0.25 for sums; with dw 2 d bytes a token.  fp32 models: about
+ * three times that, and the head rows of a piece (up to 1.5 GiB). */
 int hero_lm_loss_workspace_size(const hero_dims *dims, int vocab, int T, int with_dx, int with_dw, size_t *bytes);
 
 /*

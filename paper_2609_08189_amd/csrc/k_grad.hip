@@ -41,12 +41,12 @@ __device__ __forceinline__ int tensor_of(const GradTable& tab, uint32_t c) {
   return lo;
 }
 
-// f(chunk's first element, its elements, tensor) for the chunks of this workgroup
+// f(chunk's first element, its elements, tensor) for the chunks of workgroup b
 template <class F>
-__device__ __forceinline__ void for_chunks(const GradTable& tab, F f) {
+__device__ __forceinline__ void for_chunks(const GradTable& tab, uint32_t b, F f) {
   const uint64_t total = tab.chunk0[tab.n];
-  uint32_t c = static_cast<uint32_t>(total * blockIdx.x / gridDim.x);
-  const uint32_t end = static_cast<uint32_t>(total * (blockIdx.x + 1) / gridDim.x);
+  uint32_t c = static_cast<uint32_t>(total * b / gridDim.x);
+  const uint32_t end = static_cast<uint32_t>(total * (b + 1) / gridDim.x);
   if (c >= end) return;
   int i = tensor_of(tab, c);
   for (; c < end; ++c) {
@@ -111,14 +111,14 @@ __device__ __forceinline__ void chunk_scale(const T* g, T* o, int n, float c) {
         v[k] = static_cast<uint32_t>(lo) | (static_cast<uint32_t>(hi) << 16);
       }
     }
-    *reinterpret_cast<u32x4*>(o + static_cast<size_t>(i) * N) = v;
+    __builtin_nontemporal_store(v, reinterpret_cast<u32x4*>(o + static_cast<size_t>(i) * N));
   }
   for (int i = nv * N + threadIdx.x; i < n; i += 256) stf(o + i, ldf(g + i) * c);
 }
 
 __global__ __launch_bounds__(256) void grad_norm_kernel(GradTable tab, double* __restrict__ part) {
   double s = 0.0;
-  for_chunks(tab, [&](size_t at, int n, int i) {
+  for_chunks(tab, blockIdx.x, [&](size_t at, int n, int i) {
     if (tab.bf16[i])
       s += chunk_squares(static_cast<const bf16_t*>(tab.grad[i]) + at, n);
     else
@@ -146,7 +146,8 @@ __global__ __launch_bounds__(256) void grad_clip_kernel(GradTable tab, const dou
   if (norm && blockIdx.x == 0 && threadIdx.x == 0) *norm = static_cast<float>(v);
   // a norm that is not a number makes every gradient one, an infinite one leaves zeros and NaN
   const float c = v <= max_norm ? 1.0f : static_cast<float>(max_norm / v);
-  for_chunks(tab, [&](size_t at, int m, int i) {
+  // from the last chunk to the first: what the norm read last is still in the last-level cache
+  for_chunks(tab, gridDim.x - 1 - blockIdx.x, [&](size_t at, int m, int i) {
     if (c == 1.0f && tab.grad[i] == tab.out[i]) return;   // in place and unchanged
     if (tab.bf16[i])
       chunk_scale(static_cast<const bf16_t*>(tab.grad[i]) + at, static_cast<bf16_t*>(tab.out[i]) + at, m, c);

@@ -4,11 +4,12 @@
 //   dh = r u - h r^3 <h, u> / d,     u = w dx
 //   dw = sum over the rows of dx h r
 //
-// A row is read once into registers, by one wave (many rows) or by the four waves of a workgroup (few rows,
-// wide rows); sums are fp32, every output is rounded once.  HBM bounds both: 2 accesses an element forwards,
-// 3 backwards.  The backward's workgroups keep the gain's gradient of their rows in registers and write one
-// partial row each; a second launch adds those in order, so the result does not depend on timing.
+// A row is read once into registers, by one wave (narrow rows) or by the four waves of a workgroup; sums are
+// fp32, every output is rounded once.  HBM bounds both: 2 accesses an element forwards, 3 backwards.  For the
+// gain's gradient a workgroup (or wave) takes several rows, the next one's loads under way, keeps their sum in
+// registers and writes one partial row; a second launch adds those in order, so the result does not depend on timing.
 #include <algorithm>
+#include <type_traits>
 
 #include "hero_device.h"
 #include "hero_kernels.h"
@@ -17,8 +18,10 @@ namespace hero {
 namespace {
 
 constexpr int kNormThreads = 256;
-constexpr int kWideRow = 8192;      // widest row of one wave: 16 chunks of eight elements a lane
-constexpr int kGainGroups = 512;    // workgroups of a backward with the gain's gradient
+constexpr int kGainRows = 1024;     // most partial rows of the gain's gradient
+// A wave a row up to here: with a workgroup a row half of its threads or more would have nothing to do.  The
+// width alone decides, so that a row's sums have one order whatever the call.
+constexpr int kWaveRow = 1024;
 
 // sum over a row's WPR waves (a workgroup's, if more than one), left in every lane
 template <int WPR>
@@ -76,7 +79,6 @@ __global__ __launch_bounds__(kNormThreads) void final_norm_bwd_kernel(const T* _
                                                                       float eps, T* __restrict__ dh,
                                                                       float* __restrict__ part) {
   __shared__ float red[2][4];
-  extern __shared__ float gsum[];   // GAIN, one wave a row: d floats
   int turn = 0;
   constexpr int L = 64 * WPR;
   const int lane = WPR == 4 ? threadIdx.x : threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -88,15 +90,21 @@ __global__ __launch_bounds__(kNormThreads) void final_norm_bwd_kernel(const T* _
     for (int i = 0; i < NC; ++i)
 #pragma unroll
       for (int k = 0; k < 8; ++k) acc[i][k] = 0.f;
-  for (int t = first; t < rows; t += step) {
+  Raw8<T> v[NC], y[NC], nv[NC], ny[NC];
+  auto fetch = [&](Raw8<T>(&a)[NC], Raw8<T>(&b)[NC], int t) {
     const size_t at = static_cast<size_t>(t) * d;
-    Raw8<T> v[NC], y[NC];
 #pragma unroll
     for (int i = 0; i < NC; ++i)
       if (lane + i * L < nc) {
-        v[i].load(h + at + 8 * (lane + i * L));
-        y[i].load(dx + at + 8 * (lane + i * L));
+        a[i].load(h + at + 8 * (lane + i * L));
+        b[i].load(dx + at + 8 * (lane + i * L));
       }
+  };
+  if (first < rows) fetch(v, y, first);
+  for (int t = first; t < rows; t += step) {
+    const size_t at = static_cast<size_t>(t) * d;
+    if constexpr (GAIN)   // several rows a workgroup: the next one's loads are under way
+      if (t + step < rows) fetch(nv, ny, t + step);
     float ss = 0.f, hu = 0.f;
 #pragma unroll
     for (int i = 0; i < NC; ++i)
@@ -126,113 +134,80 @@ __global__ __launch_bounds__(kNormThreads) void final_norm_bwd_kernel(const T* _
         }
         st8(dh + at + 8 * (lane + i * L), o);
       }
+    if constexpr (GAIN)
+#pragma unroll
+      for (int i = 0; i < NC; ++i) {
+        v[i] = nv[i];
+        y[i] = ny[i];
+      }
   }
   if constexpr (GAIN) {
-    float* out = part + static_cast<size_t>(blockIdx.x) * d;
-    if constexpr (WPR == 4) {
+    float* out = part + static_cast<size_t>(first) * d;
 #pragma unroll
-      for (int i = 0; i < NC; ++i)
-        if (lane + i * L < nc) st8(out + 8 * (lane + i * L), acc[i]);
-    } else {
-      for (int q = 0; q < 4; ++q) {   // the four waves' rows, added in order
-        if (wave == q)
-#pragma unroll
-          for (int i = 0; i < NC; ++i)
-            if (lane + i * L < nc)
-#pragma unroll
-              for (int k = 0; k < 8; ++k) {
-                float* p = gsum + 8 * (lane + i * L) + k;
-                *p = q ? *p + acc[i][k] : acc[i][k];
-              }
-        __syncthreads();
-      }
-      for (int i = threadIdx.x; i < d; i += kNormThreads) out[i] = gsum[i];
-    }
+    for (int i = 0; i < NC; ++i)
+      if (lane + i * L < nc) st8(out + 8 * (lane + i * L), acc[i]);
   }
 }
 
-// out[i] = sum over the groups of part[g][i], 64 columns a workgroup, its four waves a quarter of the groups each
-__global__ __launch_bounds__(256) void gain_reduce_kernel(const float* __restrict__ part, int groups, int d,
-                                                          float* __restrict__ out) {
-  __shared__ float red[4][64];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, i = blockIdx.x * 64 + lane;
-  float s[4] = {0.f, 0.f, 0.f, 0.f};
-  const int per = (groups + 3) / 4, g1 = min(groups, (wave + 1) * per);
-  if (i < d) {
-    int g = wave * per;
-    for (; g + 4 <= g1; g += 4)
-#pragma unroll
-      for (int k = 0; k < 4; ++k) s[k] += part[static_cast<size_t>(g + k) * d + i];
-    for (; g < g1; ++g) s[0] += part[static_cast<size_t>(g) * d + i];
-  }
-  red[wave][lane] = (s[0] + s[1]) + (s[2] + s[3]);
+// out[i] = sum over the partial rows: 16 columns a workgroup, every 64th row a thread, so that few rows of few
+// columns still are many loads at once (1024 rows of 1024 columns, 64 columns a workgroup: 15 us)
+__global__ __launch_bounds__(1024) void gain_reduce_kernel(const float* __restrict__ part, int rows, int d,
+                                                           float* __restrict__ out) {
+  __shared__ float red[64][17];
+  const int c = threadIdx.x & 15, r = threadIdx.x >> 4, i = blockIdx.x * 16 + c;
+  float s = 0.f;
+#pragma unroll 16
+  for (int g = r; g < rows; g += 64) s += part[static_cast<size_t>(g) * d + i];
+  red[r][c] = s;
   __syncthreads();
-  if (wave == 0 && i < d) out[i] = (red[0][lane] + red[1][lane]) + (red[2][lane] + red[3][lane]);
+#pragma unroll
+  for (int k = 32; k > 0; k >>= 1) {
+    if (r < k) red[r][c] += red[r + k][c];
+    __syncthreads();
+  }
+  if (r == 0) out[i] = red[0][c];
 }
 
-// chunks of eight elements a lane holds: the smallest compiled count that covers the row
-int norm_chunks(int d, int wpr) { return (d / 8 + 64 * wpr - 1) / (64 * wpr); }
-
-// Few rows leave CUs idle with a wave a row, and a wave's chain of loads is four times as long as a
-// workgroup's: a row takes a whole workgroup then, and where it is wider than a wave's registers.
-bool norm_whole_group(int T, int d) { return T <= 4 * 256 || d > kWideRow; }
+// f(chunks of eight elements a lane holds, waves a row): the smallest compiled count that covers the row
+template <class F>
+void norm_shape(int d, F f) {
+  const int n = (d / 8 + 255) / 256;
+  if (d <= 512) f(std::integral_constant<int, 1>(), std::integral_constant<int, 1>());
+  else if (d <= kWaveRow) f(std::integral_constant<int, 2>(), std::integral_constant<int, 1>());
+  else if (n <= 1) f(std::integral_constant<int, 1>(), std::integral_constant<int, 4>());
+  else if (n <= 2) f(std::integral_constant<int, 2>(), std::integral_constant<int, 4>());
+  else if (n <= 3) f(std::integral_constant<int, 3>(), std::integral_constant<int, 4>());
+  else if (n <= 4) f(std::integral_constant<int, 4>(), std::integral_constant<int, 4>());
+  else f(std::integral_constant<int, 16>(), std::integral_constant<int, 4>());
+}
 
 template <typename T>
 hipError_t norm_fwd(const void* h, const void* w, int rows, int d, float eps, void* x, hipStream_t s) {
-  const T *hh = static_cast<const T*>(h), *ww = static_cast<const T*>(w);
-  T* xx = static_cast<T*>(x);
-#define HERO_NORM(NC, WPR) \
-  final_norm_kernel<T, NC, WPR><<<WPR == 4 ? rows : (rows + 3) / 4, kNormThreads, 0, s>>>(hh, ww, rows, d, eps, xx)
-  if (norm_whole_group(rows, d)) {
-    const int n = norm_chunks(d, 4);
-    if (n <= 1) HERO_NORM(1, 4);
-    else if (n <= 2) HERO_NORM(2, 4);
-    else if (n <= 4) HERO_NORM(4, 4);
-    else HERO_NORM(16, 4);
-  } else {
-    const int n = norm_chunks(d, 1);
-    if (n <= 2) HERO_NORM(2, 1);
-    else if (n <= 4) HERO_NORM(4, 1);
-    else if (n <= 8) HERO_NORM(8, 1);
-    else if (n <= 10) HERO_NORM(10, 1);
-    else HERO_NORM(16, 1);
-  }
-#undef HERO_NORM
+  norm_shape(d, [&](auto nc, auto wpr) {
+    constexpr int NC = decltype(nc)::value, WPR = decltype(wpr)::value;
+    final_norm_kernel<T, NC, WPR><<<WPR == 4 ? rows : (rows + 3) / 4, kNormThreads, 0, s>>>(
+        static_cast<const T*>(h), static_cast<const T*>(w), rows, d, eps, static_cast<T*>(x));
+  });
   return hipGetLastError();
 }
 
 template <typename T, bool GAIN>
 hipError_t norm_bwd(const void* h, const void* dx, const void* w, int rows, int d, float eps, void* dh, float* part,
                     hipStream_t s) {
-  const T *hh = static_cast<const T*>(h), *yy = static_cast<const T*>(dx), *ww = static_cast<const T*>(w);
-  T* oo = static_cast<T*>(dh);
-#define HERO_NORM(NC, WPR)                                                                                    \
-  final_norm_bwd_kernel<T, NC, WPR, GAIN>                                                                     \
-      <<<GAIN ? final_norm_bwd_groups(rows, d) : WPR == 4 ? rows : (rows + 3) / 4, kNormThreads,              \
-         GAIN && WPR == 1 ? d * 4 : 0, s>>>(hh, yy, ww, rows, d, eps, oo, part)
-  if (norm_whole_group(rows, d)) {
-    const int n = norm_chunks(d, 4);
-    if (n <= 1) HERO_NORM(1, 4);
-    else if (n <= 2) HERO_NORM(2, 4);
-    else if (n <= 4) HERO_NORM(4, 4);
-    else HERO_NORM(16, 4);
-  } else {
-    const int n = norm_chunks(d, 1);
-    if (n <= 2) HERO_NORM(2, 1);
-    else if (n <= 4) HERO_NORM(4, 1);
-    else if (n <= 8) HERO_NORM(8, 1);
-    else if (n <= 10) HERO_NORM(10, 1);
-    else HERO_NORM(16, 1);
-  }
-#undef HERO_NORM
+  norm_shape(d, [&](auto nc, auto wpr) {
+    constexpr int NC = decltype(nc)::value, WPR = decltype(wpr)::value;
+    const int n = GAIN ? final_norm_bwd_groups(rows) : rows;
+    final_norm_bwd_kernel<T, NC, WPR, GAIN><<<WPR == 4 ? n : (n + 3) / 4, kNormThreads, 0, s>>>(
+        static_cast<const T*>(h), static_cast<const T*>(dx), static_cast<const T*>(w), rows, d, eps, static_cast<T*>(dh),
+        part);
+  });
   return hipGetLastError();
 }
 
 }  // namespace
 
-int final_norm_bwd_groups(int T, int d) {
-  return std::min(norm_whole_group(T, d) ? T : (T + 3) / 4, kGainGroups);
-}
+// partial rows: a workgroup's or a wave's each, whole workgroups
+int final_norm_bwd_groups(int T) { return (std::min(T, kGainRows) + 3) / 4 * 4; }
 
 hipError_t launch_final_norm(int dtype, const void* h, const void* norm_w, int T, int d, float eps, void* x,
                              hipStream_t s) {
@@ -249,7 +224,7 @@ hipError_t launch_final_norm_bwd(int dtype, const void* h, const void* dx, const
     e = dnorm_w ? norm_bwd<float, true>(h, dx, norm_w, T, d, eps, dh, part, s)
                 : norm_bwd<float, false>(h, dx, norm_w, T, d, eps, dh, part, s);
   if (e != hipSuccess || !dnorm_w) return e;
-  gain_reduce_kernel<<<(d + 63) / 64, 256, 0, s>>>(part, final_norm_bwd_groups(T, d), d, dnorm_w);
+  gain_reduce_kernel<<<d / 16, 1024, 0, s>>>(part, final_norm_bwd_groups(T), d, dnorm_w);
   return hipGetLastError();
 }
 
