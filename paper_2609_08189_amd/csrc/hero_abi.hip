@@ -1721,7 +1721,8 @@ struct LmLayout {
   int mode;
   int chunk, n_chunks;       // rows of a chunk, chunks of T rows
   int cols, pieces, pitch;   // columns of a piece (the last takes the rest), widest piece's pitch
-  int slices, ldl;           // K slices of the logits, 0: none kept; their pitch
+  int ldl;                   // pitch of kept logits
+  int slices;                // most K slices of them, 0: none kept
   bool single;               // one piece and one chunk: dW is formed from e
   bool keep_e;
   int acc_rows, dx_depth, f32_slices;
@@ -1746,7 +1747,6 @@ LmLayout lm_layout_of(const hero_dims& d, int vocab, int T, bool dx, bool dw) {
   L.mode = d.dtype == HERO_BF16 ? hero::kLmBf16 : split ? hero::kLmSplit : hero::kLmF32;
   const bool mfma = L.mode != hero::kLmF32;
   const size_t es = L.mode == hero::kLmBf16 ? 2 : split ? 6 : 4;   // bytes of a stored e or g
-  const int ktiles = d.d / 64 * (split ? 6 : 1);
   // whole tiles of 256 columns whose e (or g) fits the piece, and whose head rows' terms do
   auto fit = [&](size_t rows) {
     size_t c = kLmPiece / rows;
@@ -1763,9 +1763,11 @@ LmLayout lm_layout_of(const hero_dims& d, int vocab, int T, bool dx, bool dw) {
   L.pitch = up(widest, 64);
   L.single = L.pieces == 1 && L.n_chunks == 1;
   L.keep_e = dx || (dw && L.single);
-  // fp32: the logits are e's buffer
-  L.slices = mfma ? hero::lm_logit_slices(L.chunk, widest, ktiles) : 1;
-  if (mfma && L.slices == 1) L.slices = 0;
+  // what the logits of every piece's width need (kLmF32: the logits are e's buffer)
+  const hero::LmParts pw = hero::lm_parts(L.mode, L.chunk, L.cols, d.d), pl = hero::lm_parts(L.mode, L.chunk, last, d.d);
+  const bool many = L.pieces > 1;
+  L.slices = std::max(many ? pw.slices : 0, pl.slices);
+  const int parts = std::max(many ? pw.parts : 0, pl.parts);
   L.ldl = mfma ? up(widest, 256) : L.pitch;
   L.dx_depth = up(narrowest, 64) / 64 * (split ? 6 : 1);
   L.f32_slices = mfma ? 1 : hero::lm_f32_slices(L.chunk, d.d, up(narrowest, 64));
@@ -1794,7 +1796,7 @@ LmLayout lm_layout_of(const hero_dims& d, int vocab, int T, bool dx, bool dw) {
   const bool share = mfma && !L.single;
   L.e = take(std::max(L.keep_e && mfma ? c * L.pitch * es : 0, share ? gb : 0));
   L.g = share ? L.e : take(gb);
-  L.part = take(mfma && !L.slices ? c * hero::lm_parts(widest) * 8 : 0);
+  L.part = take(c * parts * 8);
   L.logits = take(L.slices * c * L.ldl * 4);
   L.acc = take(L.acc_rows * w * 4);
   L.xs = take(split ? t * w * 6 : 0);
@@ -1975,14 +1977,17 @@ int hero_lm_loss(const hero_dims* dims, int vocab, int T, const void* x, const h
     p.count = a.counts + 1 + c;
     p.e = !L.keep_e ? nullptr : mfma ? ws + L.e : ws + L.logits;
     p.part = reinterpret_cast<float2*>(ws + L.part);
-    p.logits = L.slices ? floats(L.logits) : nullptr;
-    p.slices = L.slices;
     p.acc = floats(L.acc);
     for (int k = 0; k < L.pieces && e == hipSuccess; ++k) {
       p.v0 = k * L.cols;
       p.cols = lm_piece_cols(L, vocab, k);
       p.pitch = (p.cols + 63) / 64 * 64;
       p.ldl = mfma ? L.ldl : p.pitch;
+      const hero::LmParts q = hero::lm_parts(L.mode, L.chunk, p.cols, D.d);
+      p.parts = q.parts;
+      p.shift = q.shift;
+      p.slices = q.slices;
+      p.logits = q.slices ? floats(L.logits) : nullptr;
       p.first = k == 0;
       p.last = k == L.pieces - 1;
       p.ws = ws + L.ws;
@@ -2011,7 +2016,9 @@ int hero_lm_loss(const hero_dims* dims, int vocab, int T, const void* x, const h
       hipError_t y = hero::launch_lm_xT(a, xT, L.g_pitch, s);
       if (L.single) {
         if (y == hipSuccess) y = hero::launch_lm_g_of_e(a, p, g, L.g_pitch, s);
-        return y == hipSuccess ? hero::launch_lm_dw(a, 0, vocab, g, xT, L.g_pitch, out->dw, s) : y;
+        if (y != hipSuccess) return y;
+        return T <= hero::kLmFewRows ? hero::launch_lm_dw_few(a, vocab, g, xT, L.g_pitch, out->dw, s)
+                                     : hero::launch_lm_dw(a, 0, vocab, g, xT, L.g_pitch, out->dw, s);
       }
       for (int v0 = 0; v0 < vocab && y == hipSuccess; v0 += L.g_cols) {
         const int cols = std::min(L.g_cols, vocab - v0);

@@ -406,7 +406,7 @@ hipError_t launch_grad_clip(const GradTable& tab, int groups, const double* part
 //   kLmF32   fp32 model, products in fp32
 //   kLmSplit fp32 model, products of three-term operands on the bf16 matrix cores (SixTerm)
 enum LmMode { kLmBf16 = 0, kLmF32 = 1, kLmSplit = 2 };
-constexpr int kLmDxBlocks = 512, kLmDxSlices = 32;   // a plan of several K slices: most workgroups, most slices
+constexpr int kLmDxBlocks = 512, kLmDxSlices = 128;   // a plan of several K slices: most workgroups, most slices
 constexpr int kLmSmall = 1024;   // tokens of a call whose rows are found, and whose losses are added, beside other work
 
 struct LmRows {
@@ -445,16 +445,21 @@ struct LmPiece {
   bool first, last;          // of the pieces
   const int* count;          // rows of the chunk (device)
   void* e;                   // [rows_max][pitch] exp(logit - ref), zero at the target (kLmSplit: three arrays); may be null
-  float2* part;              // [rows_max][lm_parts(cols)] {reference, sum} of a row's 64-column pieces
-  float* logits;             // [slices][rows_max][ldl] partial logits instead of e and part; null: none
+  float2* part;              // [rows_max][parts] {reference, sum} of a row's parts
+  int parts, shift;          // part of column n: n >> shift; shift 0: the wave of the large products' tile that holds it
+  float* logits;             // [slices][rows_max][ldl] partial logits, for the combining pass to exponentiate; null: none
   int slices, ldl;
   const void* ws;            // kLmSplit: [3][cols][d] terms of the piece's head rows
   const void* wts;           // kLmSplit: [3][d][pitch] ... transposed
   float* acc;                // [slices of the plan][rows][d] sum over the vocabulary of e W
 };
 constexpr int kLmLogitsMax = 8192;   // columns of a piece whose logits are kept (kLmF32: of any)
-int lm_parts(int cols);
-int lm_logit_slices(int rows, int cols, int ktiles);
+constexpr int kLmFewRows = 64;       // most rows of the dW product that is all writing
+// which of the three forms the logits take: parts and shift of a row (slices 0), or K slices of kept logits
+struct LmParts {
+  int parts, shift, slices;
+};
+LmParts lm_parts(int mode, int rows, int cols, int d);
 hipError_t launch_lm_logits(const LmRows& a, const LmPiece& p, hipStream_t s);
 // the row's sums with this piece's; e in units of the row's reference after it; after the last piece its loss
 hipError_t launch_lm_combine(const LmRows& a, const LmPiece& p, hipStream_t s);
@@ -479,6 +484,8 @@ hipError_t launch_lm_g(const LmRows& a, int v0, int cols, const void* ws, const 
 hipError_t launch_lm_g_products(const LmRows& a, int v0, int cols, const void* ws, void* g, int pitch, hipStream_t s);
 // g from the e of a call of one piece and one chunk
 hipError_t launch_lm_g_of_e(const LmRows& a, const LmPiece& p, void* g, int pitch, hipStream_t s);
+// few rows (T <= kLmFewRows), one piece
+hipError_t launch_lm_dw_few(const LmRows& a, int cols, const void* g, const void* xT, int pitch, void* dw, hipStream_t s);
 hipError_t launch_lm_dw(const LmRows& a, int v0, int cols, const void* g, const void* xT, int pitch, void* dw, hipStream_t s);
 
 // out[t][r][c], t < 3: the terms of in[r][c] (row idx[r] where given, *count rows); cols a multiple of 8

@@ -2511,13 +2511,14 @@ hipError_t launch_lm_f32_logits(const float* x, const int* idx, const int* count
   // 64 x 64 tiles read a head row once for up to 64 tokens
   if (rows_max > 32 && (cols + 63) / 64 * ((rows_max + 63) / 64) >= kCUs)
     return run_f32_r<false, 4>(A, B, epi, count, rows_max, cols, d, true, s);
+  if (rows_max <= 16) return run_f32_r<false, 1>(A, B, epi, count, rows_max, cols, d, true, s);
   return run_f32<false>(A, B, epi, count, rows_max, cols, d, s);
 }
 
-// K slices of the dx product: 32 x 32 tiles that leave CUs idle share K, a slice of at least 512
+// K slices of the dx product: 32 x 32 tiles that leave CUs idle share K, a slice of at least 256
 int lm_f32_slices(int rows, int d, int K) {
   const int tiles = (rows + 31) / 32 * ((d + 31) / 32);
-  return std::max(1, std::min({4 * kCUs / std::max(tiles, 1), K / 512, 32}));
+  return std::max(1, std::min({4 * kCUs / std::max(tiles, 1), K / 256, 32}));
 }
 
 hipError_t launch_lm_f32_dx(const float* e, const int* count, int rows_max, int pitch, const float* w_t, int ld_wt, int d,
@@ -2527,6 +2528,12 @@ hipError_t launch_lm_f32_dx(const float* e, const int* count, int rows_max, int 
   if (rows_max > 32) {
     const dim3 g4((rows_max + 63) / 64, (d + 63) / 64, slices);
     lm_f32_dx<4><<<g4, 256, 0, s>>>(ARows<float>{e, nullptr, pitch}, BRows<float>{w_t, nullptr, INT_MAX, ld_wt},
+                                    EpiLmF32{acc, d, alpha, first}, count, d, pitch, Kz);
+    return hipGetLastError();
+  }
+  if (rows_max <= 16) {
+    const dim3 g1(1, (d + 15) / 16, slices);
+    lm_f32_dx<1><<<g1, 256, 0, s>>>(ARows<float>{e, nullptr, pitch}, BRows<float>{w_t, nullptr, INT_MAX, ld_wt},
                                     EpiLmF32{acc, d, alpha, first}, count, d, pitch, Kz);
     return hipGetLastError();
   }

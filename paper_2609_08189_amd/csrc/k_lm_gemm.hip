@@ -240,6 +240,69 @@ __global__ __launch_bounds__(512, 2) void lm_g_product(ARows<bf16_t> A, BRows<bf
   phase_any<false>(bm, A, B, epi, M, mt, K, n_tiles, smem, tile_of(blockIdx.x, mt * n_tiles), 0, 1);
 }
 
+// dW of few rows: little to compute and all of dW to write.  A workgroup takes 128 head rows, a wave 32 of them
+// (operand B: their g, held), and `width` columns of d (A: rows of x^T, staged in LDS, so that no load waits behind
+// a store: with both in one loop 26 rows of d = 3584 against 116669 took 303 us, so 162, 5.2 TB/s).  Rows of A are dealt out so that a lane's sixteen results are neighbours, and the four lanes of a head
+// row write 64 elements of it in whole lines.  G: groups of 32 (bf16) or 16 (fp32) tokens.
+template <typename T, int G>
+__global__ __launch_bounds__(256) void lm_dw_few(LmRows a, int cols, const T* __restrict__ g, const T* __restrict__ xT,
+                                                 int pitch, int width, T* __restrict__ dw) {
+  constexpr bool F32 = std::is_same_v<T, float>;
+  typedef std::conditional_t<F32, f32x4, bf16x8> Frag;
+  constexpr int E = F32 ? 4 : 8, ROW = 64 * G + 16;   // bytes of a staged row: 16-byte reads of 16 rows miss each other
+  __shared__ __attribute__((aligned(16))) unsigned char xs[256 * ROW];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l15 = lane & 15, q = lane >> 4;
+  const int i0 = blockIdx.y * width, di = min(width, a.d - i0);
+  for (int e = threadIdx.x; e < di * 4 * G; e += 256)
+    *reinterpret_cast<u32x4*>(xs + (e / (4 * G)) * ROW + e % (4 * G) * 16) = *reinterpret_cast<const u32x4*>(
+        reinterpret_cast<const unsigned char*>(xT + static_cast<size_t>(i0 + e / (4 * G)) * pitch) + e % (4 * G) * 16);
+  const float unit = F32 ? 1.0f : a.mean ? a.scale / static_cast<float>(max(a.counts[0], 1)) : a.scale;
+  Frag fg[2][G];
+#pragma unroll
+  for (int b = 0; b < 2; ++b)
+#pragma unroll
+    for (int k = 0; k < G; ++k)
+      fg[b][k] = *reinterpret_cast<const Frag*>(
+          g + static_cast<size_t>(min(static_cast<int>(blockIdx.x) * 128 + wave * 32 + 16 * b + l15, cols - 1)) * pitch +
+          (4 * k + q) * E);
+  __syncthreads();
+  for (int i = 0; i < di; i += 64) {
+    f32x4 acc[2][4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      acc[0][j] = acc[1][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+      const unsigned char* row = xs + (i + 16 * (l15 >> 2) + 4 * j + (l15 & 3)) * ROW;
+#pragma unroll
+      for (int k = 0; k < G; ++k) {
+        const Frag fx = *reinterpret_cast<const Frag*>(row + (4 * k + q) * 16);
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+          if constexpr (F32) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              acc[b][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(fx[e], fg[b][k][e], acc[b][j], 0, 0, 0);
+          } else {
+            acc[b][j] = mfma_op(fx, fg[b][k], acc[b][j]);
+          }
+        }
+      }
+    }
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+      const int n = blockIdx.x * 128 + wave * 32 + 16 * b + l15;
+      if (n >= cols) continue;
+      T* out = dw + static_cast<size_t>(n) * a.d + i0 + i + 16 * q;
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        float v[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[k] = unit * acc[b][2 * h + (k >> 2)][k & 3];
+        st8(out + 8 * h, v);
+      }
+    }
+  }
+}
+
 int lm_tiles(int n) { return (n + 255) / 256; }
 
 template <bool SIX>
@@ -262,7 +325,7 @@ hipError_t lm_logits(const LmRows& a, const LmPiece& p, hipStream_t s) {
   const int* tgt = a.tgt + p.m0;
   bf16_t* e = static_cast<bf16_t*>(p.e);
   const size_t term = static_cast<size_t>(p.rows_max) * p.pitch;
-  const int parts = lm_parts(p.cols);
+  const int parts = p.parts;
   if (e)
     return run_phase<false>(A, B, EpiLmExp<true, SIX>{{}, ref, tgt, p.v0, p.cols, p.pitch, e, term, p.part, parts}, p.count,
                             p.rows_max, n, K, s, false);
@@ -314,14 +377,15 @@ hipError_t lm_dw(const LmRows& a, int v0, int cols, const void* g, const void* x
 
 }  // namespace
 
-int lm_parts(int cols) { return 4 * lm_tiles(cols); }
-
-// K slices of the logits where 128-row tiles leave half of the CUs idle or more, at least four k-tiles each, unless
-// the rows are long: one workgroup takes a row of them to its exponentials (one row of 32000: 26 us, with the
-// epilogue's exponentials 5)
-int lm_logit_slices(int rows, int cols, int ktiles) {
-  const int tiles = (rows + 127) / 128 * lm_tiles(cols);
-  return 2 * tiles > kCUs || cols > kLmLogitsMax - 256 ? 1 : std::max(1, std::min(kCUs / tiles, ktiles / 4));
+// The form that the logits take: the large products with e in their epilogue; where 128-row tiles leave half of the
+// CUs idle or more and a workgroup of the combining pass holds a row, K slices of the logits, for that pass to
+// exponentiate (134 rows of d = 1536 against 1066 columns: 42 -> 31 us a call).  Longer rows gain nothing from slices:
+// 10 rows of d = 2048 against 39058 columns, 153 tiles, took 56 us so and 65 + 7 in five slices.  kLmF32: always kept.
+LmParts lm_parts(int mode, int rows, int cols, int d) {
+  if (mode == kLmF32) return cols <= kLmLogitsMax ? LmParts{0, 0, 1} : LmParts{(cols + 8191) / 8192, 13, 1};
+  const int tiles = (rows + 127) / 128 * lm_tiles(cols), ktiles = d / 64 * (mode == kLmSplit ? 6 : 1);
+  const int S = 2 * tiles > kCUs || cols > kLmLogitsMax - 256 ? 1 : std::min(kCUs / tiles, ktiles / 4);
+  return S > 1 ? LmParts{0, 0, S} : LmParts{4 * lm_tiles(cols), 0, 0};
 }
 
 hipError_t launch_lm_logits(const LmRows& a, const LmPiece& p, hipStream_t s) {
@@ -336,6 +400,24 @@ hipError_t launch_lm_dx(const LmRows& a, const LmPiece& p, const void* w_t, int 
   if (a.mode == kLmSplit) return lm_dx<true>(a, p, nullptr, 0, s);
   return launch_lm_f32_dx(static_cast<const float*>(p.e), p.count, p.rows_max, p.pitch, static_cast<const float*>(w_t) + p.v0,
                           ld_wt, a.d, a.f32_slices, a.alpha + p.m0, p.first, p.acc, s);
+}
+
+hipError_t launch_lm_dw_few(const LmRows& a, int cols, const void* g, const void* xT, int pitch, void* dw, hipStream_t s) {
+  const int gx = (cols + 127) / 128, width = gx * ((a.d + 255) / 256) >= kCUs ? 256 : 64;   // small heads: more workgroups
+  const dim3 grid(gx, (a.d + width - 1) / width);
+#define HERO_LM_DW(T, G)                                                                                       \
+  lm_dw_few<T, G><<<grid, 256, 0, s>>>(a, cols, static_cast<const T*>(g), static_cast<const T*>(xT), pitch, width, \
+                                       static_cast<T*>(dw))
+  if (a.mode == kLmBf16) {
+    if (a.T <= 32) HERO_LM_DW(bf16_t, 1);
+    else HERO_LM_DW(bf16_t, 2);
+  } else {
+    if (a.T <= 16) HERO_LM_DW(float, 1);
+    else if (a.T <= 32) HERO_LM_DW(float, 2);
+    else HERO_LM_DW(float, 4);
+  }
+#undef HERO_LM_DW
+  return hipGetLastError();
 }
 
 hipError_t launch_lm_dw(const LmRows& a, int v0, int cols, const void* g, const void* xT, int pitch, void* dw, hipStream_t s) {

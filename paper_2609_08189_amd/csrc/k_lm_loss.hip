@@ -38,7 +38,7 @@ __device__ __forceinline__ bool counts_of(const LmRows& a, int t) {
 __device__ __forceinline__ int dx_plan(const LmRows& a, int M, int lane) {
   float time = 3.0e38f;
   int best = 256 | 1 << 16;
-  for (int c = lane; c < 3 * 7; c += kWave) {   // 1, 2, 4, 8, 16, 24 or 32 slices: whole XCDs to a slice
+  for (int c = lane; c < 3 * 19; c += kWave) {   // 1, 2, 4 or 8, 16 .. 128 slices: whole XCDs to a slice
     const int bm = 256 - 64 * (c % 3), k = c / 3, S = k < 4 ? 1 << k : 8 * (k - 2), w = bm == 256 ? 125 : bm == 192 ? 100 : 75;
     const int tiles = (M + bm - 1) / bm * a.dx_tiles;
     if (S > 1 && (static_cast<long long>(S) * M > a.acc_rows || tiles * S > kLmDxBlocks || a.dx_depth < 4 * S)) continue;
@@ -284,11 +284,11 @@ __device__ __forceinline__ bool no_row(const LmRows& a, const LmPiece& p, int i)
 
 __global__ __launch_bounds__(1024) void lm_sum_kernel(LmRows a) { add_losses(a); }
 
-// The sums of a row's pieces of 64 columns, a workgroup a row.  A piece whose reference is not the row's (a logit
-// far above the target's) raises the row's: then the earlier sums, and this piece's e, are rescaled.
-__global__ __launch_bounds__(256) void lm_combine_kernel(LmRows a, LmPiece p, int parts) {
+// The sums of a row's parts, a workgroup a row.  A part whose reference is not the row's (a logit far above the
+// target's) raises the row's: then the earlier sums, and this piece's e, are rescaled.
+__global__ __launch_bounds__(256) void lm_combine_kernel(LmRows a, LmPiece p) {
   __shared__ float red[4];
-  const int i = blockIdx.x, m = p.m0 + i;
+  const int parts = p.parts, i = blockIdx.x, m = p.m0 + i;
   if (no_row(a, p, i)) return;
   const float r0 = a.ref[m];
   const float2* part = p.part + static_cast<size_t>(i) * parts;
@@ -309,11 +309,15 @@ __global__ __launch_bounds__(256) void lm_combine_kernel(LmRows a, LmPiece p, in
   if (threadIdx.x == 0) row_sums(a, p, m, r0, r, s);
   if (raised && p.e) {
     bf16_t* e = static_cast<bf16_t*>(p.e) + static_cast<size_t>(i) * p.pitch;
+    float* e32 = static_cast<float*>(p.e) + static_cast<size_t>(i) * p.pitch;
     const size_t term = a.mode == kLmSplit ? static_cast<size_t>(p.rows_max) * p.pitch : 0;
-    for (int n = threadIdx.x; n < p.pitch; n += 256) {   // the columns of wave (n & 127) / 32 of tile n / 256
+    for (int n = threadIdx.x; n < p.pitch; n += 256) {
+      const int q = p.shift ? n >> p.shift : (n >> 8) * 4 + ((n & 127) >> 5);
       // in two halves: e may be e^60 and the factor below the smallest number
-      const float f = expf(0.5f * (part[(n >> 8) * 4 + ((n & 127) >> 5)].x - r));
-      if (term == 0) {
+      const float f = expf(0.5f * (part[q].x - r));
+      if (a.mode == kLmF32) {
+        e32[n] = e32[n] * f * f;
+      } else if (term == 0) {
         e[n] = f32_to_bf16(bf16_to_f32(e[n]) * f * f);
       } else {
         float v = (bf16_to_f32(e[n]) + bf16_to_f32(e[n + term]) + bf16_to_f32(e[n + 2 * term])) * f * f;
@@ -329,12 +333,13 @@ __global__ __launch_bounds__(256) void lm_combine_kernel(LmRows a, LmPiece p, in
 
 // The logits of a piece, in K slices, to e: a workgroup a row, eight columns a thread in registers; zeros up to
 // the pitch.  One round of loads, two reductions: reading the logits once for the maximum and once for the
-// exponentials took 1088 rows of 1286 columns 11.6 us.
+// exponentials took 1088 rows of 1286 columns 11.6 us.  Long fp32 rows: a workgroup 8192 columns (grid y), which are
+// a part each for the combining pass (one row of 82971 by one workgroup: 30 us).
 template <int MODE, int NT>
 __global__ __launch_bounds__(NT) void lm_exp_kernel(LmRows a, LmPiece p) {
   __shared__ float red[16];
-  const int i = blockIdx.x, m = p.m0 + i, n = 8 * threadIdx.x;
-  if (no_row(a, p, i)) return;
+  const int i = blockIdx.x, m = p.m0 + i, n = 8 * (blockIdx.y * NT + threadIdx.x);
+  if (p.shift ? i >= *p.count : no_row(a, p, i)) return;
   const float* l = p.logits + static_cast<size_t>(i) * p.ldl + n;
   const size_t slice = static_cast<size_t>(p.rows_max) * p.ldl;
   const float r0 = a.ref[m];
@@ -366,31 +371,10 @@ __global__ __launch_bounds__(NT) void lm_exp_kernel(LmRows a, LmPiece p) {
   if (p.e && n < p.pitch)
     put8<MODE>(p.e, static_cast<size_t>(i) * p.pitch + n, static_cast<size_t>(p.rows_max) * p.pitch, v);
   s = group_reduce<NT>(s, false, red);
-  if (threadIdx.x == 0) row_sums(a, p, m, r0, r, s);
-  row_done(a, p);
-}
-
-// fp32 products, longer rows: the logits to e in place
-__global__ __launch_bounds__(1024) void lm_exp_long_kernel(LmRows a, LmPiece p) {
-  __shared__ float red[16];
-  const int i = blockIdx.x, m = p.m0 + i;
-  if (no_row(a, p, i)) return;
-  const float r0 = a.ref[m];
-  const int tgt = a.tgt[m] - p.v0;
-  float* l = p.logits + static_cast<size_t>(i) * p.ldl;
-  float top = r0;
-#pragma unroll 8
-  for (int n = threadIdx.x; n < p.cols; n += 1024) top = fmaxf(top, l[n]);
-  top = group_reduce<1024>(top, true, red);
-  const float r = top - r0 > 60.0f ? top : r0;
-  float s = 0.f;
-#pragma unroll 8
-  for (int n = threadIdx.x; n < p.pitch; n += 1024) {
-    const float v = n < p.cols && n != tgt ? expf(l[n] - r) : 0.f;
-    s += v;
-    l[n] = v;
+  if (p.shift) {
+    if (threadIdx.x == 0) p.part[static_cast<size_t>(i) * p.parts + blockIdx.y] = {r, s};
+    return;
   }
-  s = group_reduce<1024>(s, false, red);
   if (threadIdx.x == 0) row_sums(a, p, m, r0, r, s);
   row_done(a, p);
 }
@@ -557,10 +541,8 @@ template <int MODE>
 void lm_exp(const LmRows& a, const LmPiece& p, hipStream_t s) {
   if (p.pitch <= 2048)
     lm_exp_kernel<MODE, 256><<<p.rows_max, 256, 0, s>>>(a, p);
-  else if (p.pitch <= kLmLogitsMax)
-    lm_exp_kernel<MODE, 1024><<<p.rows_max, 1024, 0, s>>>(a, p);
   else
-    lm_exp_long_kernel<<<p.rows_max, 1024, 0, s>>>(a, p);   // kLmF32: the others keep no such rows
+    lm_exp_kernel<MODE, 1024><<<dim3(p.rows_max, (p.pitch + 8191) / 8192), 1024, 0, s>>>(a, p);
 }
 
 }  // namespace
@@ -590,14 +572,15 @@ hipError_t launch_lm_sum(const LmRows& a, hipStream_t s) {
 }
 
 hipError_t launch_lm_combine(const LmRows& a, const LmPiece& p, hipStream_t s) {
-  if (!p.logits)
-    lm_combine_kernel<<<p.rows_max, 256, 0, s>>>(a, p, lm_parts(p.cols));
-  else if (a.mode == kLmBf16)
-    lm_exp<kLmBf16>(a, p, s);
-  else if (a.mode == kLmF32)
-    lm_exp<kLmF32>(a, p, s);
-  else
-    lm_exp<kLmSplit>(a, p, s);
+  if (p.logits) {
+    if (a.mode == kLmBf16)
+      lm_exp<kLmBf16>(a, p, s);
+    else if (a.mode == kLmF32)
+      lm_exp<kLmF32>(a, p, s);
+    else
+      lm_exp<kLmSplit>(a, p, s);
+  }
+  if (!p.logits || p.shift) lm_combine_kernel<<<p.rows_max, 256, 0, s>>>(a, p);
   return hipGetLastError();
 }
 

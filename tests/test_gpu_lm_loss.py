@@ -33,7 +33,8 @@ def _check(c, y):
 
 SIZES = [(1, 256, 65), (1, 512, 2003), (2, 256, 127), (3, 256, 128), (17, 512, 256), (63, 256, 257), (64, 768, 320),
          (65, 256, 1000), (129, 512, 4001), (257, 256, 2003), (300, 1024, 511), (600, 256, 3001), (1025, 256, 1537),
-         (1, 256, 40001), (5, 256, 33000), (300, 256, 20011), (130, 1280, 700), (2000, 256, 8000)]
+         (1, 256, 40001), (5, 256, 33000), (300, 256, 20011), (130, 1280, 700), (2000, 256, 8000),
+         (16, 256, 9001), (17, 512, 8200), (33, 768, 8191), (64, 1024, 10007), (48, 256, 24577), (767, 256, 33333)]
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
@@ -78,12 +79,13 @@ def test_chunks_of_rows_and_pieces_of_the_vocabulary(T, d, V, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
-@pytest.mark.parametrize("T,size", [(5, 30.0), (200, 30.0), (200, 120.0)])
-def test_logits_far_above_the_target(T, size, dtype):
+@pytest.mark.parametrize("T,size,V", [(5, 30.0, 1700), (200, 30.0, 1700), (200, 120.0, 1700), (7, 30.0, 9001), (40, 120.0, 20011),
+                                      (300, 60.0, 16001)])
+def test_logits_far_above_the_target(T, size, V, dtype):
     """References move: differences of several hundred between a row's logits."""
     from tests import train_ends as E
-    print(f"case lm_loss far T={T} size={size} {dtype}", flush=True)
-    x, w, y = _inputs(T, 256, 1700, dtype, 11, keep=0.9, size=size, sure=2.0)
+    print(f"case lm_loss far T={T} size={size} V={V} {dtype}", flush=True)
+    x, w, y = _inputs(T, 256, V, dtype, 11, keep=0.9, size=size, sure=2.0)
     _check(E.Loss(x, w, y, mean=False).run(), y)
 
 
