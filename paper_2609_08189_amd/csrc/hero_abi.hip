@@ -2013,13 +2013,13 @@ int hero_lm_loss(const hero_dims* dims, int vocab, int T, const void* x, const h
   if (e == hipSuccess && dw)
     e = timed(HERO_K_LM_DW, s, [&] {
       void *g = ws + L.g, *xT = ws + L.xT;
-      hipError_t y = hero::launch_lm_xT(a, xT, L.g_pitch, s);
       if (L.single) {
-        if (y == hipSuccess) y = hero::launch_lm_g_of_e(a, p, g, L.g_pitch, s);
+        const hipError_t y = hero::launch_lm_g_of_e(a, p, g, xT, L.g_pitch, s);
         if (y != hipSuccess) return y;
-        return T <= hero::kLmFewRows ? hero::launch_lm_dw_few(a, vocab, g, xT, L.g_pitch, out->dw, s)
-                                     : hero::launch_lm_dw(a, 0, vocab, g, xT, L.g_pitch, out->dw, s);
+        return T <= hero::kLmFewRows && !split ? hero::launch_lm_dw_few(a, vocab, g, xT, L.g_pitch, out->dw, s)
+                                                 : hero::launch_lm_dw(a, 0, vocab, g, xT, L.g_pitch, out->dw, s);
       }
+      hipError_t y = hero::launch_lm_xT(a, xT, L.g_pitch, s);
       for (int v0 = 0; v0 < vocab && y == hipSuccess; v0 += L.g_cols) {
         const int cols = std::min(L.g_cols, vocab - v0);
         const float* wv = wf + static_cast<size_t>(v0) * D.d;

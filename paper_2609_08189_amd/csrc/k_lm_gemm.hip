@@ -250,7 +250,7 @@ __global__ __launch_bounds__(256) void lm_dw_few(LmRows a, int cols, const T* __
   constexpr bool F32 = std::is_same_v<T, float>;
   typedef std::conditional_t<F32, f32x4, bf16x8> Frag;
   constexpr int E = F32 ? 4 : 8, ROW = 64 * G + 16;   // bytes of a staged row: 16-byte reads of 16 rows miss each other
-  __shared__ __attribute__((aligned(16))) unsigned char xs[256 * ROW];
+  __shared__ __attribute__((aligned(16))) unsigned char xs[(G <= 4 ? 256 : 128) * ROW];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l15 = lane & 15, q = lane >> 4;
   const int i0 = blockIdx.y * width, di = min(width, a.d - i0);
   for (int e = threadIdx.x; e < di * 4 * G; e += 256)
@@ -402,8 +402,13 @@ hipError_t launch_lm_dx(const LmRows& a, const LmPiece& p, const void* w_t, int 
                           ld_wt, a.d, a.f32_slices, a.alpha + p.m0, p.first, p.acc, s);
 }
 
+// 98 rows in bf16, four groups of tokens staged: 518 us a call where the large product takes 494.  fp32: all that do not
+// take three-term operands.
+bool lm_dw_few_rows(int mode, int T) { return mode == kLmBf16 ? T <= 64 : mode == kLmF32 && T <= 128; }
+
 hipError_t launch_lm_dw_few(const LmRows& a, int cols, const void* g, const void* xT, int pitch, void* dw, hipStream_t s) {
-  const int gx = (cols + 127) / 128, width = gx * ((a.d + 255) / 256) >= kCUs ? 256 : 64;   // small heads: more workgroups
+  const bool most = a.mode != kLmBf16 && a.T > 64;   // what is staged has to fit
+  const int gx = (cols + 127) / 128, width = gx * ((a.d + 255) / 256) >= kCUs ? most ? 128 : 256 : 64;   // small heads: more workgroups
   const dim3 grid(gx, (a.d + width - 1) / width);
 #define HERO_LM_DW(T, G)                                                                                       \
   lm_dw_few<T, G><<<grid, 256, 0, s>>>(a, cols, static_cast<const T*>(g), static_cast<const T*>(xT), pitch, width, \
@@ -414,7 +419,8 @@ hipError_t launch_lm_dw_few(const LmRows& a, int cols, const void* g, const void
   } else {
     if (a.T <= 16) HERO_LM_DW(float, 1);
     else if (a.T <= 32) HERO_LM_DW(float, 2);
-    else HERO_LM_DW(float, 4);
+    else if (a.T <= 64) HERO_LM_DW(float, 4);
+    else HERO_LM_DW(float, 8);
   }
 #undef HERO_LM_DW
   return hipGetLastError();

@@ -32,8 +32,8 @@ __device__ __forceinline__ bool counts_of(const LmRows& a, int t) {
 
 // Tile height and K slices of the dx products of M rows, by one wave, a candidate a lane and turn: the time in
 // rounds of workgroups over the CUs, a round weighted by its height (as phase_rows) and by its k-tiles, of which
-// storing an fp32 tile takes about twelve, and the finishing pass's reading of all slices (125 is a k-tile of 256
-// rows, 1.45 us).  2048 rows of d = 4096 against 32768 columns: 128-row tiles in one round 443 us, 256-row tiles in
+// storing an fp32 tile takes about twelve, and the finishing pass's reading of all slices at 4 TB/s, at least 0.15 us
+// each (125 is a k-tile of 256 rows, 1.45 us).  2048 rows of d = 4096 against 32768 columns: 128-row tiles in one round 443 us, 256-row tiles in
 // two slices 399.
 __device__ __forceinline__ int dx_plan(const LmRows& a, int M, int lane) {
   float time = 3.0e38f;
@@ -43,7 +43,7 @@ __device__ __forceinline__ int dx_plan(const LmRows& a, int M, int lane) {
     const int tiles = (M + bm - 1) / bm * a.dx_tiles;
     if (S > 1 && (static_cast<long long>(S) * M > a.acc_rows || tiles * S > kLmDxBlocks || a.dx_depth < 4 * S)) continue;
     const float v = static_cast<float>((tiles * S + 255) / 256 * w) * (static_cast<float>(a.dx_depth) / S + 12.f) +
-                    static_cast<float>(S) * M * a.d * (125.f * 4.f / (1.45f * 4.0e6f));
+                    static_cast<float>(S) * (static_cast<float>(M) * a.d * (125.f * 4.f / (1.45f * 4.0e6f)) + 13.f);
     if (v < time) {
       time = v;
       best = bm | S << 16;
@@ -439,11 +439,11 @@ __device__ __forceinline__ void transpose64(In in, Out out) {
   }
 }
 
-// xT[i][m] = x[idx[m]][i], zero behind the counted rows as far as the dW product reads
+// One 64 x 64 tile of xT[i][m] = x[idx[m]][i], zero behind the counted rows as far as the dW product reads
 template <int MODE>
-__global__ __launch_bounds__(256) void lm_xT_kernel(LmRows a, void* __restrict__ xT, int pitch) {
+__device__ __forceinline__ void xT_tile(const LmRows& a, void* __restrict__ xT, int pitch, int i0, int m0) {
   typedef std::conditional_t<MODE == kLmBf16, bf16_t, float> T;
-  const int N = a.counts[0], i0 = blockIdx.x * 64, m0 = blockIdx.y * 64;
+  const int N = a.counts[0];
   if (MODE != kLmF32 && m0 >= depth_of(N)) return;
   transpose64(
       [&](int r, int c, float* v) {
@@ -458,15 +458,15 @@ __global__ __launch_bounds__(256) void lm_xT_kernel(LmRows a, void* __restrict__
       });
 }
 
-// g[n][m] = p - [n = target]: from e of the whole vocabulary (OF_E), or from fp32 logits; kLmF32: times the unit.
-// A bf16 e is divided by its row's sum and rounded a second time, which saves forming the logits again (1777
-// tokens of d = 1024, vocabulary 50257: 196 us); the target's entry is exact but for its own rounding.
+// One 64 x 64 tile of g[n][m] = p - [n = target]: from e of the whole vocabulary (OF_E), or from fp32 logits;
+// kLmF32: times the unit.  A bf16 e is divided by its row's sum and rounded a second time, which saves forming the
+// logits again (1777 tokens of d = 1024, vocabulary 50257: 196 us); the target's entry is exact but for its own rounding.
 template <int MODE, bool OF_E>
-__global__ __launch_bounds__(256) void lm_g_kernel(LmRows a, int v0, int cols, const void* __restrict__ src, int ld,
-                                                   size_t src_term, void* __restrict__ g, int pitch) {
+__device__ __forceinline__ void g_tile(const LmRows& a, int v0, int cols, const void* __restrict__ src, int ld,
+                                       size_t src_term, void* __restrict__ g, int pitch, int n0, int m0) {
   __shared__ float row[2][64];
   __shared__ int tgt[64];
-  const int N = a.counts[0], n0 = blockIdx.x * 64, m0 = blockIdx.y * 64;
+  const int N = a.counts[0];
   if (MODE != kLmF32 && m0 >= depth_of(N)) return;
   const float unit = MODE != kLmF32 ? 1.0f : a.mean ? a.scale / static_cast<float>(max(N, 1)) : a.scale;
   if (threadIdx.x < 64) {
@@ -508,6 +508,29 @@ __global__ __launch_bounds__(256) void lm_g_kernel(LmRows a, int v0, int cols, c
         if (n0 + c < cols)
           put8<MODE>(g, static_cast<size_t>(n0 + c) * pitch + m0 + r, static_cast<size_t>(cols) * pitch, v);
       });
+}
+
+template <int MODE>
+__global__ __launch_bounds__(256) void lm_xT_kernel(LmRows a, void* __restrict__ xT, int pitch) {
+  xT_tile<MODE>(a, xT, pitch, blockIdx.x * 64, blockIdx.y * 64);
+}
+
+template <int MODE>
+__global__ __launch_bounds__(256) void lm_g_kernel(LmRows a, int v0, int cols, const float* __restrict__ logits, int ld,
+                                                   void* __restrict__ g, int pitch) {
+  g_tile<MODE, false>(a, v0, cols, logits, ld, 0, g, pitch, blockIdx.x * 64, blockIdx.y * 64);
+}
+
+// both operands of the dW product of a call of one piece and one chunk: the first workgroups of a row xT, the rest g
+template <int MODE>
+__global__ __launch_bounds__(256) void lm_g_of_e_kernel(LmRows a, LmPiece p, void* __restrict__ g, void* __restrict__ xT,
+                                                        int pitch) {
+  const int nx = a.d / 64, b = blockIdx.x;
+  if (b < nx)
+    xT_tile<MODE>(a, xT, pitch, b * 64, blockIdx.y * 64);
+  else
+    g_tile<MODE, true>(a, 0, p.cols, p.e, p.pitch, static_cast<size_t>(p.rows_max) * p.pitch, g, pitch, (b - nx) * 64,
+                       blockIdx.y * 64);
 }
 
 // w_t[i][v] = w[v][i], zero from the vocabulary to the pitch (a multiple of 64)
@@ -609,19 +632,18 @@ hipError_t launch_lm_xT(const LmRows& a, void* xT, int pitch, hipStream_t s) {
 hipError_t launch_lm_g(const LmRows& a, int v0, int cols, const void* ws, const float* logits, int ldl, void* g, int pitch,
                        hipStream_t s) {
   if (a.mode != kLmF32) return launch_lm_g_products(a, v0, cols, ws, g, pitch, s);
-  lm_g_kernel<kLmF32, false><<<dim3((cols + 63) / 64, pitch / 64), 256, 0, s>>>(a, v0, cols, logits, ldl, 0, g, pitch);
+  lm_g_kernel<kLmF32><<<dim3((cols + 63) / 64, pitch / 64), 256, 0, s>>>(a, v0, cols, logits, ldl, g, pitch);
   return hipGetLastError();
 }
 
-hipError_t launch_lm_g_of_e(const LmRows& a, const LmPiece& p, void* g, int pitch, hipStream_t s) {
-  const dim3 grid((p.cols + 63) / 64, pitch / 64);
-  const size_t term = static_cast<size_t>(p.rows_max) * p.pitch;
+hipError_t launch_lm_g_of_e(const LmRows& a, const LmPiece& p, void* g, void* xT, int pitch, hipStream_t s) {
+  const dim3 grid(a.d / 64 + (p.cols + 63) / 64, pitch / 64);
   if (a.mode == kLmBf16)
-    lm_g_kernel<kLmBf16, true><<<grid, 256, 0, s>>>(a, 0, p.cols, p.e, p.pitch, term, g, pitch);
+    lm_g_of_e_kernel<kLmBf16><<<grid, 256, 0, s>>>(a, p, g, xT, pitch);
   else if (a.mode == kLmF32)
-    lm_g_kernel<kLmF32, true><<<grid, 256, 0, s>>>(a, 0, p.cols, p.e, p.pitch, term, g, pitch);
+    lm_g_of_e_kernel<kLmF32><<<grid, 256, 0, s>>>(a, p, g, xT, pitch);
   else
-    lm_g_kernel<kLmSplit, true><<<grid, 256, 0, s>>>(a, 0, p.cols, p.e, p.pitch, term, g, pitch);
+    lm_g_of_e_kernel<kLmSplit><<<grid, 256, 0, s>>>(a, p, g, xT, pitch);
   return hipGetLastError();
 }
 
