@@ -2016,8 +2016,8 @@ int hero_lm_loss(const hero_dims* dims, int vocab, int T, const void* x, const h
       if (L.single) {
         const hipError_t y = hero::launch_lm_g_of_e(a, p, g, xT, L.g_pitch, s);
         if (y != hipSuccess) return y;
-        return T <= hero::kLmFewRows && !split ? hero::launch_lm_dw_few(a, vocab, g, xT, L.g_pitch, out->dw, s)
-                                                 : hero::launch_lm_dw(a, 0, vocab, g, xT, L.g_pitch, out->dw, s);
+        return hero::lm_dw_few_rows(L.mode, T) ? hero::launch_lm_dw_few(a, vocab, g, xT, L.g_pitch, out->dw, s)
+                                               : hero::launch_lm_dw(a, 0, vocab, g, xT, L.g_pitch, out->dw, s);
       }
       hipError_t y = hero::launch_lm_xT(a, xT, L.g_pitch, s);
       for (int v0 = 0; v0 < vocab && y == hipSuccess; v0 += L.g_cols) {

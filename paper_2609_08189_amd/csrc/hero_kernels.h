@@ -454,7 +454,6 @@ struct LmPiece {
   float* acc;                // [slices of the plan][rows][d] sum over the vocabulary of e W
 };
 constexpr int kLmLogitsMax = 8192;   // columns of a piece whose logits are kept (kLmF32: of any)
-constexpr int kLmFewRows = 128;      // most rows of the dW product that is all writing
 // which of the three forms the logits take: parts and shift of a row (slices 0), or K slices of kept logits
 struct LmParts {
   int parts, shift, slices;
@@ -484,7 +483,8 @@ hipError_t launch_lm_g(const LmRows& a, int v0, int cols, const void* ws, const 
 hipError_t launch_lm_g_products(const LmRows& a, int v0, int cols, const void* ws, void* g, int pitch, hipStream_t s);
 // xT, and g from the e of a call of one piece and one chunk
 hipError_t launch_lm_g_of_e(const LmRows& a, const LmPiece& p, void* g, void* xT, int pitch, hipStream_t s);
-// few rows (T <= kLmFewRows), one piece
+// few rows, one piece
+bool lm_dw_few_rows(int mode, int T);
 hipError_t launch_lm_dw_few(const LmRows& a, int cols, const void* g, const void* xT, int pitch, void* dw, hipStream_t s);
 hipError_t launch_lm_dw(const LmRows& a, int v0, int cols, const void* g, const void* xT, int pitch, void* dw, hipStream_t s);
 
