@@ -1727,7 +1727,9 @@ struct LmLayout {
   bool keep_e;
   int acc_rows, dx_depth, f32_slices;
   int g_cols, g_pitch, g_ldl;
-  size_t idx, inv, tgt, counts, plan, done, lt, ref, sum, alpha, nll, lse, own, e, part, acc, g, xT, logits, xs, ws, wts, total;
+  int dw_slices;
+  size_t idx, inv, tgt, counts, plan, done, lt, ref, sum, alpha, nll, lse, own, e, part, acc, g, xT, logits, xs, ws, wts,
+      dw_part, total;
 };
 
 int lm_piece_cols(const LmLayout& L, int vocab, int k) { return k == L.pieces - 1 ? vocab - k * L.cols : L.cols; }
@@ -1802,6 +1804,12 @@ LmLayout lm_layout_of(const hero_dims& d, int vocab, int T, bool dx, bool dw) {
   L.xs = take(split ? t * w * 6 : 0);
   L.ws = take(split ? std::max<size_t>(widest, dw && !L.single ? std::min(L.g_cols, vocab) : 0) * w * 6 : 0);
   L.wts = take(split && dx ? static_cast<size_t>(L.pitch) * w * 6 : 0);
+  hero::LmRows r{};
+  r.mode = L.mode;
+  r.T = T;
+  r.d = d.d;
+  L.dw_slices = dw && L.single ? hero::lm_dw_slices(r, vocab) : 1;
+  L.dw_part = take(L.dw_slices > 1 ? static_cast<size_t>(L.dw_slices) * vocab * w * 4 : 0);
   L.xT = take(dw ? w * L.g_pitch * es : 0);
   if (dw && !mfma && !L.single) {   // the logits of all rows, after the loss's are done with
     const size_t need = t * L.g_ldl * 4;
@@ -2009,15 +2017,17 @@ int hero_lm_loss(const hero_dims* dims, int vocab, int T, const void* x, const h
     }
     if (e == hipSuccess && dx) e = timed(HERO_K_LM_FINISH, s, [&] { return hero::launch_lm_finish(a, p, out->dx, s); });
   }
-  if (e == hipSuccess && T > hero::kLmSmall) e = timed(HERO_K_LM_FINISH, s, [&] { return hero::launch_lm_sum(a, s); });
+  if (e == hipSuccess && T > hero::kLmCounted) e = timed(HERO_K_LM_FINISH, s, [&] { return hero::launch_lm_sum(a, s); });
   if (e == hipSuccess && dw)
     e = timed(HERO_K_LM_DW, s, [&] {
       void *g = ws + L.g, *xT = ws + L.xT;
       if (L.single) {
         const hipError_t y = hero::launch_lm_g_of_e(a, p, g, xT, L.g_pitch, s);
         if (y != hipSuccess) return y;
-        return hero::lm_dw_few_rows(L.mode, T) ? hero::launch_lm_dw_few(a, vocab, g, xT, L.g_pitch, out->dw, s)
-                                               : hero::launch_lm_dw(a, 0, vocab, g, xT, L.g_pitch, out->dw, s);
+        if (hero::lm_dw_few_rows(L.mode, T)) return hero::launch_lm_dw_few(a, vocab, g, xT, L.g_pitch, out->dw, s);
+        if (L.dw_slices == 1) return hero::launch_lm_dw(a, 0, vocab, g, xT, L.g_pitch, out->dw, s);
+        const hipError_t x = hero::launch_lm_dw_part(a, vocab, g, xT, L.g_pitch, floats(L.dw_part), L.dw_slices, s);
+        return x == hipSuccess ? hero::launch_lm_dw_sum(a, floats(L.dw_part), L.dw_slices, vocab, out->dw, s) : x;
       }
       hipError_t y = hero::launch_lm_xT(a, xT, L.g_pitch, s);
       for (int v0 = 0; v0 < vocab && y == hipSuccess; v0 += L.g_cols) {

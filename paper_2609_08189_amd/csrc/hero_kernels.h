@@ -407,7 +407,8 @@ hipError_t launch_grad_clip(const GradTable& tab, int groups, const double* part
 //   kLmSplit fp32 model, products of three-term operands on the bf16 matrix cores (SixTerm)
 enum LmMode { kLmBf16 = 0, kLmF32 = 1, kLmSplit = 2 };
 constexpr int kLmDxBlocks = 512, kLmDxSlices = 128;   // a plan of several K slices: most workgroups, most slices
-constexpr int kLmSmall = 1024;   // tokens of a call whose rows are found, and whose losses are added, beside other work
+constexpr int kLmSmall = 8192;   // tokens of a call whose rows are found in the launch that takes their targets' logits
+constexpr int kLmCounted = 256;  // ... whose losses are added by the last row to finish
 
 struct LmRows {
   int mode, T, d, vocab;
@@ -418,7 +419,7 @@ struct LmRows {
   int* tgt;                  // [T] target of a row
   int* counts;               // [0] all rows; [1 + c] rows of chunk c
   int* plan;                 // [chunks] tile height of the dx products, K slices << 16
-  unsigned* done;            // rows whose loss is known (at most kLmSmall tokens)
+  unsigned* done;            // rows whose loss is known (at most kLmCounted tokens)
   float* lt;                 // [T] target's logit
   float* ref;                // [T] reference logit of the row's sums
   float* sum;                // [T] sum over the vocabulary but the target of exp(logit - ref)
@@ -435,7 +436,7 @@ struct LmRows {
 };
 // the rows, their targets' logits; everything else that a call starts from
 hipError_t launch_lm_rows(const LmRows& a, hipStream_t s);
-// loss[0] of more than kLmSmall tokens (of fewer: the last combine)
+// loss[0] of more than kLmCounted tokens (of fewer: the last combine)
 hipError_t launch_lm_sum(const LmRows& a, hipStream_t s);
 
 // One piece of the vocabulary for one chunk of rows: columns [v0, v0 + cols), rows [m0, m0 + rows_max)
@@ -483,6 +484,16 @@ hipError_t launch_lm_g(const LmRows& a, int v0, int cols, const void* ws, const 
 hipError_t launch_lm_g_products(const LmRows& a, int v0, int cols, const void* ws, void* g, int pitch, hipStream_t s);
 // xT, and g from the e of a call of one piece and one chunk
 hipError_t launch_lm_g_of_e(const LmRows& a, const LmPiece& p, void* g, void* xT, int pitch, hipStream_t s);
+// dW in K slices part [slices][cols][d] (one piece); 1: not worth it
+int lm_dw_slices(const LmRows& a, int cols);
+// the slices that a product over `depth` tokens has work for, four k-tiles each
+__host__ __device__ inline int lm_dw_slices_of(int slices, int depth) {
+  const int most = depth / 256;
+  return most < 1 ? 1 : most < slices ? most : slices;
+}
+hipError_t launch_lm_dw_part(const LmRows& a, int cols, const void* g, const void* xT, int pitch, float* part, int slices,
+                             hipStream_t s);
+hipError_t launch_lm_dw_sum(const LmRows& a, const float* part, int slices, int cols, void* dw, hipStream_t s);
 // few rows, one piece
 bool lm_dw_few_rows(int mode, int T);
 hipError_t launch_lm_dw_few(const LmRows& a, int cols, const void* g, const void* xT, int pitch, void* dw, hipStream_t s);

@@ -240,6 +240,24 @@ __global__ __launch_bounds__(512, 2) void lm_g_product(ARows<bf16_t> A, BRows<bf
   phase_any<false>(bm, A, B, epi, M, mt, K, n_tiles, smem, tile_of(blockIdx.x, mt * n_tiles), 0, 1);
 }
 
+// The dW product in K slices, for heads of few tiles: slice z into part + z M d
+template <bool SIX>
+struct EpiLmDwPart : EpiLmAcc<true, SIX> {
+  static constexpr bool kDeviceDepth = true;
+  const int* count;
+  __device__ __forceinline__ int depth() const { return lm_depth(count); }
+};
+template <class Epi>
+__global__ __launch_bounds__(512, 2) void lm_dw_part_kernel(ARows<bf16_t> A, BRows<bf16_t> B, Epi epi, int M, int n_tiles,
+                                                            int slices) {
+  using C = Phase<128, false>;
+  __shared__ __attribute__((aligned(1024))) unsigned char smem[2 * C::STAGE];
+  const int S = lm_dw_slices_of(slices, epi.depth()), z = blockIdx.y, mt = row_tiles(M, M, C::BM);
+  if (z >= S) return;
+  epi.out += static_cast<size_t>(z) * M * epi.ld;
+  phase_tile<C>(A, B, epi, M, mt, 0, n_tiles, smem, tile_of(blockIdx.x, mt * n_tiles), z, S);
+}
+
 // dW of few rows: little to compute and all of dW to write.  A workgroup takes 128 head rows, a wave 32 of them
 // (operand B: their g, held), and `width` columns of d (A: rows of x^T, staged in LDS, so that no load waits behind
 // a store: with both in one loop 26 rows of d = 3584 against 116669 took 303 us, so 162, 5.2 TB/s).  Rows of A are dealt out so that a lane's sixteen results are neighbours, and the four lanes of a head
@@ -400,6 +418,36 @@ hipError_t launch_lm_dx(const LmRows& a, const LmPiece& p, const void* w_t, int 
   if (a.mode == kLmSplit) return lm_dx<true>(a, p, nullptr, 0, s);
   return launch_lm_f32_dx(static_cast<const float*>(p.e), p.count, p.rows_max, p.pitch, static_cast<const float*>(w_t) + p.v0,
                           ld_wt, a.d, a.f32_slices, a.alpha + p.m0, p.first, p.acc, s);
+}
+
+// K slices of a dW product whose 128-row tiles leave half of the CUs idle or more: a k-tile takes 0.62 us, the slices
+// are written and read at 4.5 TB/s, by one more launch (3300 rows of d = 512 against 1097 columns, 18 tiles: 78 -> 68 us a
+// call)
+int lm_dw_slices(const LmRows& a, int cols) {
+  const int tiles = (cols + 127) / 128 * (a.d / 256);
+  if (a.mode == kLmF32 || 2 * tiles > kCUs) return 1;
+  const double k = (a.mode == kLmSplit ? 6 : 1) * (a.T / 64) * 0.62, part = 8.0 * cols * a.d / 4.5e6;
+  int best = 1;
+  double time = k;
+  for (int S = 2; S <= kCUs / tiles; ++S)
+    if (k / S + part * S + 5.0 < time) {
+      time = k / S + part * S + 5.0;
+      best = S;
+    }
+  return lm_dw_slices_of(best, a.T);
+}
+
+hipError_t launch_lm_dw_part(const LmRows& a, int cols, const void* g, const void* xT, int pitch, float* part, int slices,
+                             hipStream_t s) {
+  ARows<bf16_t> A{static_cast<const bf16_t*>(g), nullptr, pitch, nullptr, 0, static_cast<size_t>(cols) * pitch};
+  BRows<bf16_t> B{static_cast<const bf16_t*>(xT), nullptr, INT_MAX, pitch, INT_MAX, nullptr, static_cast<size_t>(a.d) * pitch};
+  const int n_tiles = a.d / 256;
+  const dim3 grid(((cols + 127) / 128 * n_tiles + 7) / 8 * 8, slices);
+  if (a.mode == kLmSplit)
+    lm_dw_part_kernel<<<grid, 512, 0, s>>>(A, B, EpiLmDwPart<true>{{{}, part, a.d, nullptr}, a.counts}, cols, n_tiles, slices);
+  else
+    lm_dw_part_kernel<<<grid, 512, 0, s>>>(A, B, EpiLmDwPart<false>{{{}, part, a.d, nullptr}, a.counts}, cols, n_tiles, slices);
+  return hipGetLastError();
 }
 
 // 98 rows in bf16, four groups of tokens staged: 518 us a call where the large product takes 494.  fp32: all that do not

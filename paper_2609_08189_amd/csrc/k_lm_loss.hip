@@ -26,10 +26,6 @@ namespace {
 
 constexpr int kRowsThreads = 1024;
 
-__device__ __forceinline__ bool counts_of(const LmRows& a, int t) {
-  return static_cast<unsigned>(a.targets[t]) < static_cast<unsigned>(a.vocab);
-}
-
 // Tile height and K slices of the dx products of M rows, by one wave, a candidate a lane and turn: the time in
 // rounds of workgroups over the CUs, a round weighted by its height (as phase_rows) and by its k-tiles, of which
 // storing an fp32 tile takes about twelve, and the finishing pass's reading of all slices at 4 TB/s, at least 0.15 us
@@ -93,17 +89,28 @@ __device__ __forceinline__ void target_row(const LmRows& a, int m, int t, int la
   }
 }
 
-// Up to kLmSmall tokens in one launch: every workgroup counts all targets for itself, four a thread, and
-// takes the four tokens of one of its threads, a wave each.
-template <typename T>
+// four targets from t on; those behind the last token do not count
+__device__ __forceinline__ int4 four_targets(const LmRows& a, int t) {
+  if (t + 4 <= a.T) return *reinterpret_cast<const int4*>(a.targets + t);
+  return int4{t < a.T ? a.targets[t] : -1, t + 1 < a.T ? a.targets[t + 1] : -1, t + 2 < a.T ? a.targets[t + 2] : -1, -1};
+}
+__device__ __forceinline__ int counted(const LmRows& a, int y) {
+  return static_cast<unsigned>(y) < static_cast<unsigned>(a.vocab);
+}
+
+// Up to kLmSmall tokens in one launch: every workgroup counts all targets for itself, F fours a thread, and takes
+// one of them, a token a wave.  5719 tokens of d = 512: 6 us, where a compaction by one workgroup and a second launch
+// took 14 + 4.
+template <typename T, int F>
 __global__ __launch_bounds__(256) void lm_rows_small_kernel(LmRows a) {
   __shared__ int wsum[4], rank[4], live[4];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, t0 = 4 * threadIdx.x;
-  int in[4], n = 0;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, t0 = 4 * F * threadIdx.x;
+  int in[F], n = 0;   // four bits a four
 #pragma unroll
-  for (int k = 0; k < 4; ++k) {
-    in[k] = t0 + k < a.T && counts_of(a, t0 + k);
-    n += in[k];
+  for (int f = 0; f < F; ++f) {
+    const int4 y = four_targets(a, t0 + 4 * f);
+    in[f] = counted(a, y.x) | counted(a, y.y) << 1 | counted(a, y.z) << 2 | counted(a, y.w) << 3;
+    n += __popc(in[f]);
   }
   int incl = n;
 #pragma unroll
@@ -114,14 +121,20 @@ __global__ __launch_bounds__(256) void lm_rows_small_kernel(LmRows a) {
   if (lane == 63) wsum[wave] = incl;
   __syncthreads();
   const int total = wsum[0] + wsum[1] + wsum[2] + wsum[3];
-  if (threadIdx.x == blockIdx.x) {
+  if (threadIdx.x == blockIdx.x / F) {
     int m = incl - n;
     for (int w = 0; w < wave; ++w) m += wsum[w];
+    int bits = 0;
+#pragma unroll
+    for (int f = 0; f < F; ++f) {
+      if (f < static_cast<int>(blockIdx.x % F)) m += __popc(in[f]);
+      if (f == static_cast<int>(blockIdx.x % F)) bits = in[f];
+    }
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
-      live[k] = in[k];
+      live[k] = bits >> k & 1;
       rank[k] = m;
-      m += in[k];
+      m += live[k];
     }
   }
   if (blockIdx.x == 0) {
@@ -155,10 +168,14 @@ __global__ __launch_bounds__(256) void lm_rows_small_kernel(LmRows a) {
 __global__ __launch_bounds__(kRowsThreads) void lm_rows_kernel(LmRows a) {
   __shared__ int wsum[kRowsThreads / kWave];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int per = (a.T + kRowsThreads - 1) / kRowsThreads;
+  const int per = (a.T + 4 * kRowsThreads - 1) / (4 * kRowsThreads) * 4;   // whole 16-byte loads
   const int t0 = min(a.T, static_cast<int>(threadIdx.x) * per), t1 = min(a.T, t0 + per);
   int n = 0;
-  for (int t = t0; t < t1; ++t) n += counts_of(a, t);
+#pragma unroll 4
+  for (int t = t0; t < t1; t += 4) {
+    const int4 y = four_targets(a, t);
+    n += counted(a, y.x) + counted(a, y.y) + counted(a, y.z) + counted(a, y.w);
+  }
   int incl = n;
 #pragma unroll
   for (int off = 1; off < kWave; off <<= 1) {
@@ -172,13 +189,20 @@ __global__ __launch_bounds__(kRowsThreads) void lm_rows_kernel(LmRows a) {
     if (w < wave) m += wsum[w];
     total += wsum[w];
   }
-  for (int t = t0; t < t1; ++t) {
-    const bool in = counts_of(a, t);
-    a.inv[t] = in ? m : -1;
-    if (in)
-      a.idx[m++] = t;
-    else if (a.token_loss)
-      a.token_loss[t] = 0.f;
+#pragma unroll 2
+  for (int t = t0; t < t1; t += 4) {
+    const int4 y = four_targets(a, t);
+    const int v[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      if (t + k >= t1) break;
+      const bool in = counted(a, v[k]);
+      a.inv[t + k] = in ? m : -1;
+      if (in)
+        a.idx[m++] = t + k;
+      else if (a.token_loss)
+        a.token_loss[t + k] = 0.f;
+    }
   }
   for (int i = total + threadIdx.x; i < a.T; i += kRowsThreads) a.idx[i] = 0;   // rows that no result uses
   if (threadIdx.x == 0) a.counts[0] = total;
@@ -263,10 +287,11 @@ __device__ __forceinline__ void add_losses(const LmRows& a) {
 // Few tokens: the workgroup whose row is the last to finish adds the losses, in row order, which saves a launch
 // (5 us of 36 where one token is scored).  Without rows the first workgroup writes the loss of none.  Only the
 // rows' losses pass between workgroups, by device-scope stores that are waited for before the count: a
-// device-scope fence instead writes every dirty line of the XCD's cache back (1000 rows 55 us, so 20).
+// device-scope fence instead writes every dirty line of the XCD's cache back (1000 rows 55 us, so 20).  More rows
+// than kLmCounted queue at the counter for longer than a launch takes.
 __device__ __forceinline__ void row_done(const LmRows& a, const LmPiece& p) {
   __shared__ bool last;
-  if (a.T > kLmSmall || !p.last) return;
+  if (a.T > kLmCounted || !p.last) return;
   if (threadIdx.x == 0) {
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     last = __hip_atomic_fetch_add(a.done, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) + 1 ==
@@ -278,7 +303,7 @@ __device__ __forceinline__ void row_done(const LmRows& a, const LmPiece& p) {
 }
 __device__ __forceinline__ bool no_row(const LmRows& a, const LmPiece& p, int i) {
   if (i < *p.count) return false;
-  if (i == 0 && p.last && a.T <= kLmSmall && threadIdx.x == 0) a.loss[0] = 0.f;
+  if (i == 0 && p.last && a.T <= kLmCounted && threadIdx.x == 0) a.loss[0] = 0.f;
   return true;
 }
 
@@ -417,6 +442,27 @@ __global__ __launch_bounds__(256) void lm_finish_kernel(LmRows a, LmPiece p, int
 // ---------------------------------------------------------------------------
 
 __device__ __forceinline__ int depth_of(int rows) { return max(128, (rows + 63) / 64 * 64); }
+
+// dW from its K slices (as many as the counted tokens have work for), eight elements a thread
+template <typename T>
+__global__ __launch_bounds__(256) void lm_dw_sum_kernel(LmRows a, const float* __restrict__ part, int slices, size_t n,
+                                                        T* __restrict__ dw) {
+  const size_t e = (static_cast<size_t>(blockIdx.x) * 256 + threadIdx.x) * 8;
+  if (e >= n) return;
+  const int S = lm_dw_slices_of(slices, depth_of(a.counts[0]));
+  const float unit = a.mean ? a.scale / static_cast<float>(max(a.counts[0], 1)) : a.scale;
+  float o[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+  for (int z = 0; z < S; ++z) {
+    float v[8];
+    ld8(part + z * n + e, v);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) o[k] += v[k];
+  }
+#pragma unroll
+  for (int k = 0; k < 8; ++k) o[k] *= unit;
+  st8(dw + e, o);
+}
 
 // in(r, c, v): the eight values of row r at columns c .. c + 7; out(c, r, v): those of column c at rows r ..
 template <class In, class Out>
@@ -573,10 +619,19 @@ void lm_exp(const LmRows& a, const LmPiece& p, hipStream_t s) {
 hipError_t launch_lm_rows(const LmRows& a, hipStream_t s) {
   const bool b16 = a.mode == kLmBf16;
   if (a.T <= kLmSmall) {
-    if (b16)
-      lm_rows_small_kernel<bf16_t><<<(a.T + 3) / 4, 256, 0, s>>>(a);
+    const int grid = (a.T + 3) / 4;
+#define HERO_LM_ROWS(F)                                                    \
+  (b16 ? lm_rows_small_kernel<bf16_t, F><<<grid, 256, 0, s>>>(a) \
+       : lm_rows_small_kernel<float, F><<<grid, 256, 0, s>>>(a))
+    if (a.T <= 1024)
+      HERO_LM_ROWS(1);
+    else if (a.T <= 2048)
+      HERO_LM_ROWS(2);
+    else if (a.T <= 4096)
+      HERO_LM_ROWS(4);
     else
-      lm_rows_small_kernel<float><<<(a.T + 3) / 4, 256, 0, s>>>(a);
+      HERO_LM_ROWS(8);
+#undef HERO_LM_ROWS
     return hipGetLastError();
   }
   lm_rows_kernel<<<1, kRowsThreads, 0, s>>>(a);
@@ -644,6 +699,16 @@ hipError_t launch_lm_g_of_e(const LmRows& a, const LmPiece& p, void* g, void* xT
     lm_g_of_e_kernel<kLmF32><<<grid, 256, 0, s>>>(a, p, g, xT, pitch);
   else
     lm_g_of_e_kernel<kLmSplit><<<grid, 256, 0, s>>>(a, p, g, xT, pitch);
+  return hipGetLastError();
+}
+
+hipError_t launch_lm_dw_sum(const LmRows& a, const float* part, int slices, int cols, void* dw, hipStream_t s) {
+  const size_t n = static_cast<size_t>(cols) * a.d;
+  const int blocks = static_cast<int>((n / 8 + 255) / 256);
+  if (a.mode == kLmBf16)
+    lm_dw_sum_kernel<bf16_t><<<blocks, 256, 0, s>>>(a, part, slices, n, static_cast<bf16_t*>(dw));
+  else
+    lm_dw_sum_kernel<float><<<blocks, 256, 0, s>>>(a, part, slices, n, static_cast<float*>(dw));
   return hipGetLastError();
 }
 

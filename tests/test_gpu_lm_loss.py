@@ -34,7 +34,8 @@ def _check(c, y):
 SIZES = [(1, 256, 65), (1, 512, 2003), (2, 256, 127), (3, 256, 128), (17, 512, 256), (63, 256, 257), (64, 768, 320),
          (65, 256, 1000), (129, 512, 4001), (257, 256, 2003), (300, 1024, 511), (600, 256, 3001), (1025, 256, 1537),
          (1, 256, 40001), (5, 256, 33000), (300, 256, 20011), (130, 1280, 700), (2000, 256, 8000),
-         (16, 256, 9001), (17, 512, 8200), (33, 768, 8191), (64, 1024, 10007), (48, 256, 24577), (100, 1280, 9000), (128, 512, 2000), (127, 256, 40000), (767, 256, 33333)]
+         (16, 256, 9001), (17, 512, 8200), (33, 768, 8191), (64, 1024, 10007), (48, 256, 24577), (100, 1280, 9000), (128, 512, 2000), (127, 256, 40000),
+         (3000, 512, 1100), (1300, 256, 600), (767, 256, 33333)]
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
@@ -70,7 +71,7 @@ def test_fp32_widths_of_half_a_tile(T, d, V):
 
 
 @pytest.mark.parametrize("T,d,V,dtype", [(8192 + 9, 256, 16384 + 300, "bf16"), (8192 + 9, 256, 5376 + 200, "f32"),
-                                         (8192, 256, 32768 + 77, "bf16"), (2000, 384, 33800, "f32"), (1500, 256, 30000, "f32")])
+                                         (8192, 256, 32768 + 77, "bf16"), (5001, 256, 9000, "bf16"), (8193, 256, 3000, "bf16"), (40000, 256, 300, "bf16"), (2000, 384, 33800, "f32"), (1500, 256, 30000, "f32")])
 def test_chunks_of_rows_and_pieces_of_the_vocabulary(T, d, V, dtype):
     from tests import train_ends as E
     print(f"case lm_loss pieces T={T} d={d} V={V} {dtype}", flush=True)
@@ -149,7 +150,7 @@ def test_tokens_that_do_not_count(dtype):
 def test_one_counted_token_anywhere():
     from tests import train_ends as E
     x, w, _ = _inputs(2500, 256, 600, "bf16", 2)
-    for t in (0, 1, 1023, 1024, 2499):
+    for t in (0, 1, 7, 1023, 1024, 2049, 2499):
         print(f"case lm_loss one counted token {t}", flush=True)
         y = np.full(2500, -1)
         y[t] = 599
