@@ -1790,11 +1790,12 @@ LmLayout lm_layout_of(const hero_dims& d, int vocab, int T, bool dx, bool dw) {
   L.nll = take(t * 4);
   L.lse = take(t * 4);
   L.own = take(t * 4);
-  L.g_pitch = mfma ? std::max(128, up(T, 64)) : up(T, 64);
+  const bool few = L.single && hero::lm_dw_few_rows(L.mode, T);   // no two k-tiles there, but in bf16 two terms of g
+  L.g_pitch = mfma && !few ? std::max(128, up(T, 64)) : up(T, 64);
   L.g_cols = L.single ? vocab : fit(static_cast<size_t>(L.g_pitch));
   L.g_ldl = up(std::min(L.g_cols, vocab), 64);
   // of several pieces or chunks, e is done with when g is formed (kLmF32: e is the logits')
-  const size_t gb = dw ? static_cast<size_t>(std::min(L.g_cols, vocab)) * L.g_pitch * es : 0;
+  const size_t gb = dw ? static_cast<size_t>(std::min(L.g_cols, vocab)) * L.g_pitch * (few && mfma ? 2 * es : es) : 0;
   const bool share = mfma && !L.single;
   L.e = take(std::max(L.keep_e && mfma ? c * L.pitch * es : 0, share ? gb : 0));
   L.g = share ? L.e : take(gb);

@@ -259,7 +259,7 @@ __global__ __launch_bounds__(512, 2) void lm_dw_part_kernel(ARows<bf16_t> A, BRo
 }
 
 // dW of few rows: little to compute and all of dW to write.  A workgroup takes 128 head rows, a wave 32 of them
-// (operand B: their g, held), and `width` columns of d (A: rows of x^T, staged in LDS, so that no load waits behind
+// (operand B: their g, held; bf16: two terms of it), and `width` columns of d (A: rows of x^T, staged in LDS, so that no load waits behind
 // a store: with both in one loop 26 rows of d = 3584 against 116669 took 303 us, so 162, 5.2 TB/s).  Rows of A are dealt out so that a lane's sixteen results are neighbours, and the four lanes of a head
 // row write 64 elements of it in whole lines.  G: groups of 32 (bf16) or 16 (fp32) tokens.
 template <typename T, int G>
@@ -275,14 +275,17 @@ __global__ __launch_bounds__(256) void lm_dw_few(LmRows a, int cols, const T* __
     *reinterpret_cast<u32x4*>(xs + (e / (4 * G)) * ROW + e % (4 * G) * 16) = *reinterpret_cast<const u32x4*>(
         reinterpret_cast<const unsigned char*>(xT + static_cast<size_t>(i0 + e / (4 * G)) * pitch) + e % (4 * G) * 16);
   const float unit = F32 ? 1.0f : a.mean ? a.scale / static_cast<float>(max(a.counts[0], 1)) : a.scale;
-  Frag fg[2][G];
+  constexpr int TERMS = F32 ? 1 : 2;   // of g
+  Frag fg[2][G][TERMS];
 #pragma unroll
   for (int b = 0; b < 2; ++b)
 #pragma unroll
     for (int k = 0; k < G; ++k)
-      fg[b][k] = *reinterpret_cast<const Frag*>(
-          g + static_cast<size_t>(min(static_cast<int>(blockIdx.x) * 128 + wave * 32 + 16 * b + l15, cols - 1)) * pitch +
-          (4 * k + q) * E);
+#pragma unroll
+      for (int t = 0; t < TERMS; ++t)
+        fg[b][k][t] = *reinterpret_cast<const Frag*>(
+            g + (static_cast<size_t>(t) * cols + min(static_cast<int>(blockIdx.x) * 128 + wave * 32 + 16 * b + l15, cols - 1)) * pitch +
+            (4 * k + q) * E);
   __syncthreads();
   for (int i = 0; i < di; i += 64) {
     f32x4 acc[2][4];
@@ -298,9 +301,10 @@ __global__ __launch_bounds__(256) void lm_dw_few(LmRows a, int cols, const T* __
           if constexpr (F32) {
 #pragma unroll
             for (int e = 0; e < 4; ++e)
-              acc[b][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(fx[e], fg[b][k][e], acc[b][j], 0, 0, 0);
+              acc[b][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(fx[e], fg[b][k][0][e], acc[b][j], 0, 0, 0);
           } else {
-            acc[b][j] = mfma_op(fx, fg[b][k], acc[b][j]);
+            acc[b][j] = mfma_op(fx, fg[b][k][1], acc[b][j]);
+            acc[b][j] = mfma_op(fx, fg[b][k][0], acc[b][j]);
           }
         }
       }

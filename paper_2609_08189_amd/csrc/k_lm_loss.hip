@@ -216,8 +216,8 @@ __global__ __launch_bounds__(256) void lm_targets_kernel(LmRows a) {
   if (m < a.counts[0]) target_row<T>(a, m, a.idx[m], threadIdx.x & 63);
 }
 
-// eight values of a row: bf16, fp32, or three bf16 terms
-template <int MODE>
+// eight values of a row: bf16, fp32, or so many bf16 terms
+template <int MODE, int TERMS = MODE == kLmSplit ? 3 : 1>
 __device__ __forceinline__ void put8(void* base, size_t at, size_t term, const float* v) {
   if constexpr (MODE == kLmF32) {
     st8(static_cast<float*>(base) + at, v);
@@ -225,7 +225,7 @@ __device__ __forceinline__ void put8(void* base, size_t at, size_t term, const f
     float r[8];
 #pragma unroll
     for (int k = 0; k < 8; ++k) r[k] = v[k];
-    for (int t = 0; t < (MODE == kLmSplit ? 3 : 1); ++t) {
+    for (int t = 0; t < TERMS; ++t) {
       st8(static_cast<bf16_t*>(base) + at + t * term, r);
 #pragma unroll
       for (int k = 0; k < 8; ++k) r[k] -= bf16_to_f32(f32_to_bf16(r[k]));
@@ -507,7 +507,9 @@ __device__ __forceinline__ void xT_tile(const LmRows& a, void* __restrict__ xT, 
 // One 64 x 64 tile of g[n][m] = p - [n = target]: from e of the whole vocabulary (OF_E), or from fp32 logits;
 // kLmF32: times the unit.  A bf16 e is divided by its row's sum and rounded a second time, which saves forming the
 // logits again (1777 tokens of d = 1024, vocabulary 50257: 196 us); the target's entry is exact but for its own rounding.
-template <int MODE, bool OF_E>
+// TWO (few rows): two bf16 terms.  With few tokens the rounding of a target's p - 1 is one factor on all of a row of
+// dW and does not average out: dW of one token was off by up to 2.4 times its output's rounding, so by 1.4.
+template <int MODE, bool OF_E, bool TWO = false>
 __device__ __forceinline__ void g_tile(const LmRows& a, int v0, int cols, const void* __restrict__ src, int ld,
                                        size_t src_term, void* __restrict__ g, int pitch, int n0, int m0) {
   __shared__ float row[2][64];
@@ -552,7 +554,8 @@ __device__ __forceinline__ void g_tile(const LmRows& a, int v0, int cols, const 
       },
       [&](int c, int r, const float* v) {
         if (n0 + c < cols)
-          put8<MODE>(g, static_cast<size_t>(n0 + c) * pitch + m0 + r, static_cast<size_t>(cols) * pitch, v);
+          put8<MODE, TWO ? 2 : MODE == kLmSplit ? 3 : 1>(g, static_cast<size_t>(n0 + c) * pitch + m0 + r,
+                                                         static_cast<size_t>(cols) * pitch, v);
       });
 }
 
@@ -568,14 +571,14 @@ __global__ __launch_bounds__(256) void lm_g_kernel(LmRows a, int v0, int cols, c
 }
 
 // both operands of the dW product of a call of one piece and one chunk: the first workgroups of a row xT, the rest g
-template <int MODE>
+template <int MODE, bool TWO>
 __global__ __launch_bounds__(256) void lm_g_of_e_kernel(LmRows a, LmPiece p, void* __restrict__ g, void* __restrict__ xT,
                                                         int pitch) {
   const int nx = a.d / 64, b = blockIdx.x;
   if (b < nx)
     xT_tile<MODE>(a, xT, pitch, b * 64, blockIdx.y * 64);
   else
-    g_tile<MODE, true>(a, 0, p.cols, p.e, p.pitch, static_cast<size_t>(p.rows_max) * p.pitch, g, pitch, (b - nx) * 64,
+    g_tile<MODE, true, TWO>(a, 0, p.cols, p.e, p.pitch, static_cast<size_t>(p.rows_max) * p.pitch, g, pitch, (b - nx) * 64,
                        blockIdx.y * 64);
 }
 
@@ -693,12 +696,14 @@ hipError_t launch_lm_g(const LmRows& a, int v0, int cols, const void* ws, const 
 
 hipError_t launch_lm_g_of_e(const LmRows& a, const LmPiece& p, void* g, void* xT, int pitch, hipStream_t s) {
   const dim3 grid(a.d / 64 + (p.cols + 63) / 64, pitch / 64);
-  if (a.mode == kLmBf16)
-    lm_g_of_e_kernel<kLmBf16><<<grid, 256, 0, s>>>(a, p, g, xT, pitch);
+  if (a.mode == kLmBf16 && lm_dw_few_rows(a.mode, a.T))
+    lm_g_of_e_kernel<kLmBf16, true><<<grid, 256, 0, s>>>(a, p, g, xT, pitch);
+  else if (a.mode == kLmBf16)
+    lm_g_of_e_kernel<kLmBf16, false><<<grid, 256, 0, s>>>(a, p, g, xT, pitch);
   else if (a.mode == kLmF32)
-    lm_g_of_e_kernel<kLmF32><<<grid, 256, 0, s>>>(a, p, g, xT, pitch);
+    lm_g_of_e_kernel<kLmF32, false><<<grid, 256, 0, s>>>(a, p, g, xT, pitch);
   else
-    lm_g_of_e_kernel<kLmSplit><<<grid, 256, 0, s>>>(a, p, g, xT, pitch);
+    lm_g_of_e_kernel<kLmSplit, false><<<grid, 256, 0, s>>>(a, p, g, xT, pitch);
   return hipGetLastError();
 }
 
