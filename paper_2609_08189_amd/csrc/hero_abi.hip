@@ -1714,7 +1714,8 @@ constexpr int kLmHeadRows = 1 << 17;         // head rows of a product, which ad
 
 // fp32 models: from so many tokens on the products of three-term operands are faster than those on the fp32 matrix
 // cores, which read operands without LDS: the head's terms cost a pass over it (4 bytes read, 6 written an
-// element), a row 2 d operations at 75 against 230 TFLOP/s.
+// element), a row 2 d operations at 75 against 230 TFLOP/s.  With dx, d = 1024, 30000 columns: 64 tokens 281 us so, 153
+// in fp32; 127 tokens 304 and 249; 255 tokens 341 and 436; 500 tokens with dW too 667 and 1333.
 constexpr int kLmSplitRows = 128;
 
 struct LmLayout {
@@ -1860,7 +1861,7 @@ int hero_final_norm_backward_workspace_size(const hero_dims* dims, int T, size_t
   if (st != HERO_OK) return st;
   if (T <= 0) return HERO_E_DIM;
   if (dims->d > hero::kNormWidest) return HERO_E_UNSUPPORTED;
-  *bytes = align_up(static_cast<size_t>(hero::final_norm_bwd_groups(T)) * dims->d * 4);
+  *bytes = align_up(static_cast<size_t>(hero::final_norm_bwd_groups(T, dims->d)) * dims->d * 4);
   return HERO_OK;
 }
 

@@ -374,10 +374,10 @@ hipError_t launch_to_f32_transpose(int dtype, const void* in, int R, int C, int 
 hipError_t launch_skip_penalty(const float* gates, int L_R, int batch, int seq, float alpha, float* loss,
                                float* dgates, hipStream_t s);
 
-// Final RMSNorm and its backward (k_norm.hip); part: final_norm_bwd_groups(T) d floats, used when
+// Final RMSNorm and its backward (k_norm.hip); part: final_norm_bwd_groups(T, d) d floats, used when
 // dnorm_w is wanted.  d <= kNormWidest.
 constexpr int kNormWidest = 32768;
-int final_norm_bwd_groups(int T);
+int final_norm_bwd_groups(int T, int d);
 hipError_t launch_final_norm(int dtype, const void* h, const void* norm_w, int T, int d, float eps, void* x,
                              hipStream_t s);
 hipError_t launch_final_norm_bwd(int dtype, const void* h, const void* dx, const void* norm_w, int T, int d, float eps,

@@ -404,19 +404,30 @@ __global__ __launch_bounds__(NT) void lm_exp_kernel(LmRows a, LmPiece p) {
   row_done(a, p);
 }
 
-// dx of a token: 2048 columns a workgroup, eight a thread, the K slices added in order
+// dx: 2048 columns a workgroup, eight a thread, the K slices added in order.  A call of one chunk takes a token a
+// workgroup; of several, a row of the chunk, and with the last chunk the tokens without a row behind those.
 template <typename T>
-__global__ __launch_bounds__(256) void lm_finish_kernel(LmRows a, LmPiece p, int last_chunk, T* __restrict__ dx) {
-  const int t = blockIdx.x, c = 8 * (blockIdx.y * blockDim.x + threadIdx.x);
+__global__ __launch_bounds__(256) void lm_finish_kernel(LmRows a, LmPiece p, T* __restrict__ dx) {
+  const int b = blockIdx.x, c = 8 * (blockIdx.y * blockDim.x + threadIdx.x);
   if (c >= a.d) return;
-  const int m = a.inv[t];
+  int t = b, m = 0;
+  if (a.n_chunks == 1) {
+    m = a.inv[t];
+  } else if (b < p.rows_max) {
+    if (b >= *p.count) return;
+    m = p.m0 + b;
+    t = a.idx[m];
+  } else {
+    t = b - p.rows_max;
+    if (a.inv[t] >= 0) return;
+    m = -1;
+  }
   T* out = dx + static_cast<size_t>(t) * a.d + c;
   if (m < 0) {
     const float zero[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    if (last_chunk) st8(out, zero);
+    st8(out, zero);
     return;
   }
-  if (m < p.m0 || m >= p.m0 + p.rows_max) return;
   const int S = a.plan[p.chunk] >> 16;
   const size_t stride = static_cast<size_t>(*p.count) * a.d;
   const float* acc = p.acc + static_cast<size_t>(m - p.m0) * a.d + c;
@@ -667,12 +678,12 @@ hipError_t launch_lm_combine(const LmRows& a, const LmPiece& p, hipStream_t s) {
 
 hipError_t launch_lm_finish(const LmRows& a, const LmPiece& p, void* dx, hipStream_t s) {
   const int nt = std::min(256, (a.d / 8 + 63) / 64 * 64);
-  const dim3 grid(a.T, (a.d / 8 + nt - 1) / nt);
-  const int last = p.chunk == a.n_chunks - 1;
+  const int rows = a.n_chunks == 1 ? a.T : p.chunk == a.n_chunks - 1 ? p.rows_max + a.T : p.rows_max;
+  const dim3 grid(rows, (a.d / 8 + nt - 1) / nt);
   if (a.mode == kLmBf16)
-    lm_finish_kernel<bf16_t><<<grid, nt, 0, s>>>(a, p, last, static_cast<bf16_t*>(dx));
+    lm_finish_kernel<bf16_t><<<grid, nt, 0, s>>>(a, p, static_cast<bf16_t*>(dx));
   else
-    lm_finish_kernel<float><<<grid, nt, 0, s>>>(a, p, last, static_cast<float*>(dx));
+    lm_finish_kernel<float><<<grid, nt, 0, s>>>(a, p, static_cast<float*>(dx));
   return hipGetLastError();
 }
 

@@ -18,7 +18,9 @@ namespace hero {
 namespace {
 
 constexpr int kNormThreads = 256;
-constexpr int kGainRows = 1024;     // most partial rows of the gain's gradient
+// Most partial rows of the gain's gradient: a workgroup each (8192 x 5120: 512, 1024, 2048 of them 74, 66, 78 us) or a
+// wave (30000 x 512: 63, 36, 28).
+constexpr int kGainRows = 1024, kGainWaveRows = 2048;
 // A wave a row up to here: with a workgroup a row half of its threads or more would have nothing to do.  The
 // width alone decides, so that a row's sums have one order whatever the call.
 constexpr int kWaveRow = 1024;
@@ -196,7 +198,7 @@ hipError_t norm_bwd(const void* h, const void* dx, const void* w, int rows, int 
                     hipStream_t s) {
   norm_shape(d, [&](auto nc, auto wpr) {
     constexpr int NC = decltype(nc)::value, WPR = decltype(wpr)::value;
-    const int n = GAIN ? final_norm_bwd_groups(rows) : rows;
+    const int n = GAIN ? final_norm_bwd_groups(rows, d) : rows;
     final_norm_bwd_kernel<T, NC, WPR, GAIN><<<WPR == 4 ? n : (n + 3) / 4, kNormThreads, 0, s>>>(
         static_cast<const T*>(h), static_cast<const T*>(dx), static_cast<const T*>(w), rows, d, eps, static_cast<T*>(dh),
         part);
@@ -207,7 +209,9 @@ hipError_t norm_bwd(const void* h, const void* dx, const void* w, int rows, int 
 }  // namespace
 
 // partial rows: a workgroup's or a wave's each, whole workgroups
-int final_norm_bwd_groups(int T) { return (std::min(T, kGainRows) + 3) / 4 * 4; }
+int final_norm_bwd_groups(int T, int d) {
+  return (std::min(T, d <= kWaveRow ? kGainWaveRows : kGainRows) + 3) / 4 * 4;
+}
 
 hipError_t launch_final_norm(int dtype, const void* h, const void* norm_w, int T, int d, float eps, void* x,
                              hipStream_t s) {
@@ -224,7 +228,7 @@ hipError_t launch_final_norm_bwd(int dtype, const void* h, const void* dx, const
     e = dnorm_w ? norm_bwd<float, true>(h, dx, norm_w, T, d, eps, dh, part, s)
                 : norm_bwd<float, false>(h, dx, norm_w, T, d, eps, dh, part, s);
   if (e != hipSuccess || !dnorm_w) return e;
-  gain_reduce_kernel<<<d / 16, 1024, 0, s>>>(part, final_norm_bwd_groups(T), d, dnorm_w);
+  gain_reduce_kernel<<<d / 16, 1024, 0, s>>>(part, final_norm_bwd_groups(T, d), d, dnorm_w);
   return hipGetLastError();
 }
 
