@@ -455,7 +455,9 @@ struct LmPiece {
   float* acc;                // [slices of the plan][rows][d] sum over the vocabulary of e W
 };
 constexpr int kLmLogitsMax = 8192;   // columns of a piece whose logits are kept (kLmF32: of any)
-// which of the three forms the logits take: parts and shift of a row (slices 0), or K slices of kept logits
+constexpr int kLmFewRows = 64;       // bf16 rows that the head streams past at once,
+constexpr long long kLmFewHead = 80000000;   // and elements of such a head
+// which of the forms the logits take: parts and shift of a row (slices 0), or K slices of kept logits
 struct LmParts {
   int parts, shift, slices;
 };

@@ -2515,6 +2515,14 @@ hipError_t launch_lm_f32_logits(const float* x, const int* idx, const int* count
   return run_f32<false>(A, B, epi, count, rows_max, cols, d, s);
 }
 
+// Tile of the dx product: 64 x 64 where such tiles and K slices give half of the CUs work or more, so that W^T is read
+// once (58 rows of d = 768 against 5068 columns, 228 workgroups: 46 us a call, on 32 x 32 49); narrower tiles have the
+// shorter chains (64 rows of d = 256 against 2003 columns, 32 workgroups: 44 us a call, on 32 x 32 38).
+static int lm_f32_tile(int rows, int d, int slices) {
+  if (rows <= 16) return 1;
+  return rows > 32 && (rows + 63) / 64 * ((d + 63) / 64) * slices >= kCUs / 2 ? 4 : 2;
+}
+
 // K slices of the dx product: 32 x 32 tiles that leave CUs idle share K, a slice of at least 256
 int lm_f32_slices(int rows, int d, int K) {
   const int tiles = (rows + 31) / 32 * ((d + 31) / 32);
@@ -2524,21 +2532,15 @@ int lm_f32_slices(int rows, int d, int K) {
 hipError_t launch_lm_f32_dx(const float* e, const int* count, int rows_max, int pitch, const float* w_t, int ld_wt, int d,
                             int slices, const float* alpha, bool first, float* acc, hipStream_t s) {
   const int Kz = (pitch + slices * 16 - 1) / (slices * 16) * 16;
-  const dim3 grid((rows_max + 31) / 32, (d + 31) / 32, slices);
-  if (rows_max > 32) {
-    const dim3 g4((rows_max + 63) / 64, (d + 63) / 64, slices);
-    lm_f32_dx<4><<<g4, 256, 0, s>>>(ARows<float>{e, nullptr, pitch}, BRows<float>{w_t, nullptr, INT_MAX, ld_wt},
-                                    EpiLmF32{acc, d, alpha, first}, count, d, pitch, Kz);
-    return hipGetLastError();
+  const ARows<float> A{e, nullptr, pitch};
+  const BRows<float> B{w_t, nullptr, INT_MAX, ld_wt};
+  const EpiLmF32 epi{acc, d, alpha, first};
+  const auto grid = [&](int R) { return dim3((rows_max + 16 * R - 1) / (16 * R), (d + 16 * R - 1) / (16 * R), slices); };
+  switch (lm_f32_tile(rows_max, d, slices)) {
+    case 1: lm_f32_dx<1><<<grid(1), 256, 0, s>>>(A, B, epi, count, d, pitch, Kz); break;
+    case 2: lm_f32_dx<2><<<grid(2), 256, 0, s>>>(A, B, epi, count, d, pitch, Kz); break;
+    default: lm_f32_dx<4><<<grid(4), 256, 0, s>>>(A, B, epi, count, d, pitch, Kz); break;
   }
-  if (rows_max <= 16) {
-    const dim3 g1(1, (d + 15) / 16, slices);
-    lm_f32_dx<1><<<g1, 256, 0, s>>>(ARows<float>{e, nullptr, pitch}, BRows<float>{w_t, nullptr, INT_MAX, ld_wt},
-                                    EpiLmF32{acc, d, alpha, first}, count, d, pitch, Kz);
-    return hipGetLastError();
-  }
-  lm_f32_dx<2><<<grid, 256, 0, s>>>(ARows<float>{e, nullptr, pitch}, BRows<float>{w_t, nullptr, INT_MAX, ld_wt},
-                                    EpiLmF32{acc, d, alpha, first}, count, d, pitch, Kz);
   return hipGetLastError();
 }
 

@@ -325,6 +325,137 @@ __global__ __launch_bounds__(256) void lm_dw_few(LmRows a, int cols, const T* __
   }
 }
 
+// ---------------------------------------------------------------------------
+// Logits of few rows: the head streams past all of them at once.  A workgroup takes 128 head rows and every row of
+// x (up to 16 TB), a ring of NS k-tiles in LDS, NS - 1 of them in flight, so that two workgroups a CU keep some 100 KB
+// under way: on the large products' tiles, of which small heads have too few, two k-tiles of 125 CUs drew 2.9 TB/s.
+// Operand A: 32 head rows a wave, B: the rows of x.  One barrier a k-tile: past it every wave has the tile's loads of
+// all waves, and none reads the tile before any more, whose place the next loads take.
+// ---------------------------------------------------------------------------
+template <int TB, int NS, bool STORE>
+__global__ __launch_bounds__(256) void lm_logits_few(LmRows a, LmPiece p) {
+  constexpr int BV = 128, BX = 16 * TB, STAGE = (BV + BX) * ROWB;
+  constexpr int XL = TB < 4 ? 1 : 2;               // loads a wave of x (TB 1: two waves repeat the others')
+  constexpr int L = 4 + XL;
+  __shared__ __attribute__((aligned(1024))) unsigned char smem[NS * STAGE];
+  const int M = *p.count;
+  if (M == 0) return;
+  const int lane = threadIdx.x & 63, l15 = lane & 15, q = lane >> 4, rsub = lane >> 3;
+  const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) >> 6);
+  const int v0 = blockIdx.x * BV;
+  const unsigned char* w = reinterpret_cast<const unsigned char*>(static_cast<const bf16_t*>(a.w) + static_cast<size_t>(p.v0) * a.d);
+  const unsigned char* x = static_cast<const unsigned char*>(a.x);
+  uint32_t w_off[4], x_off[XL];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int r = 8 * (4 * i + wave) + rsub, ch = (lane & 7) ^ ((r >> 1) & 7);
+    w_off[i] = static_cast<uint32_t>(min(v0 + r, p.cols - 1)) * static_cast<uint32_t>(a.d * 2) + ch * 16;
+  }
+  const auto x_block = [&](int i) { return (4 * i + wave) % (2 * TB); };   // of eight rows
+#pragma unroll
+  for (int i = 0; i < XL; ++i) {
+    const int r = 8 * x_block(i) + rsub, ch = (lane & 7) ^ ((r >> 1) & 7);
+    x_off[i] = static_cast<uint32_t>(a.idx[p.m0 + min(r, M - 1)]) * static_cast<uint32_t>(a.d * 2) + ch * 16;
+  }
+  const int nkt = a.d / BK;
+  auto issue = [&](int kt) {
+    unsigned char* st = smem + kt % NS * STAGE;
+    const uint32_t kb = static_cast<uint32_t>(kt) * ROWB;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) load_lds16(w + kb + w_off[i], st + (4 * i + wave) * 1024);
+#pragma unroll
+    for (int i = 0; i < XL; ++i) load_lds16(x + kb + x_off[i], st + BV * ROWB + x_block(i) * 1024);
+  };
+  f32x4 acc[2][TB];
+#pragma unroll
+  for (int f = 0; f < 2; ++f)
+#pragma unroll
+    for (int b = 0; b < TB; ++b) acc[f][b] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int k = 0; k < NS - 1; ++k) issue(k);       // d >= 256: four k-tiles at least
+  static_assert(NS <= 5, "the first loads are of tiles that exist");
+  for (int kt = 0; kt < nkt; ++kt) {
+    // this wave's loads of tile kt have landed (NS - 2 tiles behind it may be in flight; near the end all have)
+    if (kt + NS - 1 <= nkt)
+      wait_vm_lgkm<(NS - 2) * L>();
+    else
+      wait_vm_lgkm<0>();
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_sched_barrier(0);
+    if (kt + NS - 1 < nkt) issue(kt + NS - 1);
+    const unsigned char* st = smem + kt % NS * STAGE;
+#pragma unroll
+    for (int ks = 0; ks < 2; ++ks) {
+      const int c = in_chunk<16>(ks, lane);
+      bf16x8 fw[2], fx[TB];
+#pragma unroll
+      for (int f = 0; f < 2; ++f) fw[f] = *reinterpret_cast<const bf16x8*>(st + swz(wave * 32 + 16 * f + l15, c));
+#pragma unroll
+      for (int b = 0; b < TB; ++b) fx[b] = *reinterpret_cast<const bf16x8*>(st + BV * ROWB + swz(16 * b + l15, c));
+#pragma unroll
+      for (int f = 0; f < 2; ++f)
+#pragma unroll
+        for (int b = 0; b < TB; ++b) acc[f][b] = mfma_op(fw[f], fx[b], acc[f][b]);
+    }
+  }
+  // every wave is past its last reads; the ring's memory holds the columns' maxima and sums now
+  asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+  __syncthreads();
+  float* top = reinterpret_cast<float*>(smem);     // [4][BX]
+  float* sums = top + 4 * BX;
+  const int n0 = v0 + wave * 32 + 4 * q;           // lane: columns n0 + 16 f + r of row 16 b + l15
+#pragma unroll
+  for (int b = 0; b < TB; ++b) {
+    float mx = -INFINITY;
+#pragma unroll
+    for (int f = 0; f < 2; ++f)
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+        if (n0 + 16 * f + r < p.cols) mx = fmaxf(mx, acc[f][b][r]);
+    mx = fmaxf(mx, __shfl_xor(mx, 16, kWave));
+    mx = fmaxf(mx, __shfl_xor(mx, 32, kWave));
+    if (q == 0) top[wave * BX + 16 * b + l15] = mx;
+  }
+  __syncthreads();
+  float ref[TB];
+#pragma unroll
+  for (int b = 0; b < TB; ++b) {
+    const int m = 16 * b + l15, mc = p.m0 + min(m, M - 1);
+    const float r0 = a.ref[mc];
+    const float t = fmaxf(fmaxf(top[m], top[BX + m]), fmaxf(top[2 * BX + m], top[3 * BX + m]));
+    ref[b] = t - r0 > kLmAbove ? t : r0;
+    const int tgt = a.tgt[mc] - p.v0 - n0;
+    float s = 0.f;
+#pragma unroll
+    for (int f = 0; f < 2; ++f) {
+      uint32_t o[2];
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int k = 16 * f + r;
+        const float v = n0 + k < p.cols && k != tgt ? __expf(acc[f][b][r] - ref[b]) : 0.f;
+        s += v;
+        const uint32_t h = f32_to_bf16(v);
+        o[r >> 1] = r & 1 ? o[r >> 1] | h << 16 : h;
+      }
+      if constexpr (STORE)
+        if (m < M && n0 + 16 * f < p.pitch)
+          *reinterpret_cast<uint2*>(static_cast<bf16_t*>(p.e) + static_cast<size_t>(m) * p.pitch + n0 + 16 * f) = uint2{o[0], o[1]};
+    }
+    s += __shfl_xor(s, 16, kWave);
+    s += __shfl_xor(s, 32, kWave);
+    if (q == 0) sums[wave * BX + m] = s;
+  }
+  __syncthreads();
+  if (wave == 0 && q == 0)
+#pragma unroll
+    for (int b = 0; b < TB; ++b) {
+      const int m = 16 * b + l15;
+      if (m < M)
+        p.part[static_cast<size_t>(m) * p.parts + blockIdx.x] = {
+            ref[b], (sums[m] + sums[BX + m]) + (sums[2 * BX + m] + sums[3 * BX + m])};
+    }
+}
+
 int lm_tiles(int n) { return (n + 255) / 256; }
 
 template <bool SIX>
@@ -401,16 +532,35 @@ hipError_t lm_dw(const LmRows& a, int v0, int cols, const void* g, const void* x
 
 // The form that the logits take: the large products with e in their epilogue; where 128-row tiles leave half of the
 // CUs idle or more and a workgroup of the combining pass holds a row, K slices of the logits, for that pass to
-// exponentiate (134 rows of d = 1536 against 1066 columns: 42 -> 31 us a call).  Longer rows gain nothing from slices:
+// exponentiate (134 rows of d = 1536 against 1066 columns: 42 -> 31 us a call).  Few rows against a head of up to
+// 160 MB: the streaming form (3 rows of d = 768 against 77287 columns 43 -> 34 us a call, 8 of 2048 against 9000
+// 48 -> 37); larger heads draw 5.6 TB/s on the large tiles and 4.8 there (16 rows of 4096 against 128256: 185 and 222 us).
+// Longer rows gain nothing from slices:
 // 10 rows of d = 2048 against 39058 columns, 153 tiles, took 56 us so and 65 + 7 in five slices.  kLmF32: always kept.
 LmParts lm_parts(int mode, int rows, int cols, int d) {
   if (mode == kLmF32) return cols <= kLmLogitsMax ? LmParts{0, 0, 1} : LmParts{(cols + 8191) / 8192, 13, 1};
   const int tiles = (rows + 127) / 128 * lm_tiles(cols), ktiles = d / 64 * (mode == kLmSplit ? 6 : 1);
   const int S = 2 * tiles > kCUs || cols > kLmLogitsMax - 256 ? 1 : std::min(kCUs / tiles, ktiles / 4);
-  return S > 1 ? LmParts{0, 0, S} : LmParts{4 * lm_tiles(cols), 0, 0};
+  if (S > 1) return {0, 0, S};
+  if (mode == kLmBf16 && rows <= kLmFewRows && static_cast<long long>(cols) * d <= kLmFewHead) return {(cols + 127) / 128, 7, 0};
+  return {4 * lm_tiles(cols), 0, 0};
 }
 
 hipError_t launch_lm_logits(const LmRows& a, const LmPiece& p, hipStream_t s) {
+  if (a.mode == kLmBf16 && p.shift) {   // the streaming form
+    const int grid = (p.cols + 127) / 128;
+#define HERO_LM_FEW(TB, NS)                                      \
+  (p.e ? lm_logits_few<TB, NS, true><<<grid, 256, 0, s>>>(a, p) \
+       : lm_logits_few<TB, NS, false><<<grid, 256, 0, s>>>(a, p))
+    if (p.rows_max <= 16)
+      HERO_LM_FEW(1, 4);
+    else if (p.rows_max <= 32)
+      HERO_LM_FEW(2, 4);
+    else
+      HERO_LM_FEW(4, 3);
+#undef HERO_LM_FEW
+    return hipGetLastError();
+  }
   if (a.mode == kLmBf16) return lm_logits<false>(a, p, s);
   if (a.mode == kLmSplit) return lm_logits<true>(a, p, s);
   return launch_lm_f32_logits(static_cast<const float*>(a.x), a.idx + p.m0, p.count, p.rows_max,

@@ -151,19 +151,19 @@ __global__ __launch_bounds__(kNormThreads) void final_norm_bwd_kernel(const T* _
   }
 }
 
-// out[i] = sum over the partial rows: 16 columns a workgroup, every 64th row a thread, so that few rows of few
-// columns still are many loads at once (1024 rows of 1024 columns, 64 columns a workgroup: 15 us)
+// out[i] = sum over the partial rows: 32 columns (a whole line) a workgroup, every 32nd row a thread, so that few
+// rows of few columns still are many loads at once (1024 rows of 1024 columns, 64 columns a workgroup of four waves: 15 us)
 __global__ __launch_bounds__(1024) void gain_reduce_kernel(const float* __restrict__ part, int rows, int d,
                                                            float* __restrict__ out) {
-  __shared__ float red[64][17];
-  const int c = threadIdx.x & 15, r = threadIdx.x >> 4, i = blockIdx.x * 16 + c;
+  __shared__ float red[32][33];
+  const int c = threadIdx.x & 31, r = threadIdx.x >> 5, i = blockIdx.x * 32 + c;
   float s = 0.f;
 #pragma unroll 16
-  for (int g = r; g < rows; g += 64) s += part[static_cast<size_t>(g) * d + i];
+  for (int g = r; g < rows; g += 32) s += part[static_cast<size_t>(g) * d + i];
   red[r][c] = s;
   __syncthreads();
 #pragma unroll
-  for (int k = 32; k > 0; k >>= 1) {
+  for (int k = 16; k > 0; k >>= 1) {
     if (r < k) red[r][c] += red[r + k][c];
     __syncthreads();
   }
@@ -228,7 +228,7 @@ hipError_t launch_final_norm_bwd(int dtype, const void* h, const void* dx, const
     e = dnorm_w ? norm_bwd<float, true>(h, dx, norm_w, T, d, eps, dh, part, s)
                 : norm_bwd<float, false>(h, dx, norm_w, T, d, eps, dh, part, s);
   if (e != hipSuccess || !dnorm_w) return e;
-  gain_reduce_kernel<<<d / 16, 1024, 0, s>>>(part, final_norm_bwd_groups(T, d), d, dnorm_w);
+  gain_reduce_kernel<<<d / 32, 1024, 0, s>>>(part, final_norm_bwd_groups(T, d), d, dnorm_w);
   return hipGetLastError();
 }
 

@@ -35,7 +35,7 @@ SIZES = [(1, 256, 65), (1, 512, 2003), (2, 256, 127), (3, 256, 128), (17, 512, 2
          (65, 256, 1000), (129, 512, 4001), (257, 256, 2003), (300, 1024, 511), (600, 256, 3001), (1025, 256, 1537),
          (1, 256, 40001), (5, 256, 33000), (300, 256, 20011), (130, 1280, 700), (2000, 256, 8000),
          (16, 256, 9001), (17, 512, 8200), (33, 768, 8191), (64, 1024, 10007), (48, 256, 24577), (100, 1280, 9000), (128, 512, 2000), (127, 256, 40000),
-         (3000, 512, 1100), (1300, 256, 600), (767, 256, 33333)]
+         (3000, 512, 1100), (1300, 256, 600), (40, 256, 140001), (767, 256, 33333)]
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
