@@ -476,9 +476,11 @@ __global__ __launch_bounds__(256) void lm_dw_sum_kernel(LmRows a, const float* _
 }
 
 // in(r, c, v): the eight values of row r at columns c .. c + 7; out(c, r, v): those of column c at rows r ..
+// The kernel owns the tile: with one in each of the two transposes that share a launch half as many workgroups fit a
+// CU (1777 tokens of 50257 columns: 63 us, with the one about 47).
+typedef float Tile64[64][65];
 template <class In, class Out>
-__device__ __forceinline__ void transpose64(In in, Out out) {
-  __shared__ float tile[64][65];
+__device__ __forceinline__ void transpose64(Tile64& tile, In in, Out out) {
 #pragma unroll
   for (int q = threadIdx.x; q < 512; q += 256) {
     float v[8];
@@ -498,11 +500,13 @@ __device__ __forceinline__ void transpose64(In in, Out out) {
 
 // One 64 x 64 tile of xT[i][m] = x[idx[m]][i], zero behind the counted rows as far as the dW product reads
 template <int MODE>
-__device__ __forceinline__ void xT_tile(const LmRows& a, void* __restrict__ xT, int pitch, int i0, int m0) {
+__device__ __forceinline__ void xT_tile(Tile64& tile, const LmRows& a, void* __restrict__ xT, int pitch, int i0,
+                                        int m0) {
   typedef std::conditional_t<MODE == kLmBf16, bf16_t, float> T;
   const int N = a.counts[0];
   if (MODE != kLmF32 && m0 >= depth_of(N)) return;
   transpose64(
+      tile,
       [&](int r, int c, float* v) {
         if (m0 + r < N) {
           ld8(static_cast<const T*>(a.x) + static_cast<size_t>(a.idx[m0 + r]) * a.d + i0 + c, v);
@@ -521,8 +525,8 @@ __device__ __forceinline__ void xT_tile(const LmRows& a, void* __restrict__ xT, 
 // TWO (few rows): two bf16 terms.  With few tokens the rounding of a target's p - 1 is one factor on all of a row of
 // dW and does not average out: dW of one token was off by up to 2.4 times its output's rounding, so by 1.4.
 template <int MODE, bool OF_E, bool TWO = false>
-__device__ __forceinline__ void g_tile(const LmRows& a, int v0, int cols, const void* __restrict__ src, int ld,
-                                       size_t src_term, void* __restrict__ g, int pitch, int n0, int m0) {
+__device__ __forceinline__ void g_tile(Tile64& tile, const LmRows& a, int v0, int cols, const void* __restrict__ src,
+                                       int ld, size_t src_term, void* __restrict__ g, int pitch, int n0, int m0) {
   __shared__ float row[2][64];
   __shared__ int tgt[64];
   const int N = a.counts[0];
@@ -538,6 +542,7 @@ __device__ __forceinline__ void g_tile(const LmRows& a, int v0, int cols, const 
   }
   __syncthreads();
   transpose64(
+      tile,
       [&](int r, int c, float* v) {
         if (m0 + r >= N || n0 + c >= ld) {
           for (int k = 0; k < 8; ++k) v[k] = 0.f;
@@ -572,24 +577,27 @@ __device__ __forceinline__ void g_tile(const LmRows& a, int v0, int cols, const 
 
 template <int MODE>
 __global__ __launch_bounds__(256) void lm_xT_kernel(LmRows a, void* __restrict__ xT, int pitch) {
-  xT_tile<MODE>(a, xT, pitch, blockIdx.x * 64, blockIdx.y * 64);
+  __shared__ Tile64 tile;
+  xT_tile<MODE>(tile, a, xT, pitch, blockIdx.x * 64, blockIdx.y * 64);
 }
 
 template <int MODE>
 __global__ __launch_bounds__(256) void lm_g_kernel(LmRows a, int v0, int cols, const float* __restrict__ logits, int ld,
                                                    void* __restrict__ g, int pitch) {
-  g_tile<MODE, false>(a, v0, cols, logits, ld, 0, g, pitch, blockIdx.x * 64, blockIdx.y * 64);
+  __shared__ Tile64 tile;
+  g_tile<MODE, false>(tile, a, v0, cols, logits, ld, 0, g, pitch, blockIdx.x * 64, blockIdx.y * 64);
 }
 
 // both operands of the dW product of a call of one piece and one chunk: the first workgroups of a row xT, the rest g
 template <int MODE, bool TWO>
 __global__ __launch_bounds__(256) void lm_g_of_e_kernel(LmRows a, LmPiece p, void* __restrict__ g, void* __restrict__ xT,
                                                         int pitch) {
+  __shared__ Tile64 tile;
   const int nx = a.d / 64, b = blockIdx.x;
   if (b < nx)
-    xT_tile<MODE>(a, xT, pitch, b * 64, blockIdx.y * 64);
+    xT_tile<MODE>(tile, a, xT, pitch, b * 64, blockIdx.y * 64);
   else
-    g_tile<MODE, true, TWO>(a, 0, p.cols, p.e, p.pitch, static_cast<size_t>(p.rows_max) * p.pitch, g, pitch, (b - nx) * 64,
+    g_tile<MODE, true, TWO>(tile, a, 0, p.cols, p.e, p.pitch, static_cast<size_t>(p.rows_max) * p.pitch, g, pitch, (b - nx) * 64,
                        blockIdx.y * 64);
 }
 
@@ -597,8 +605,10 @@ __global__ __launch_bounds__(256) void lm_g_of_e_kernel(LmRows a, LmPiece p, voi
 template <typename T>
 __global__ __launch_bounds__(256) void lm_head_kernel(const T* __restrict__ w, int vocab, int d, T* __restrict__ w_t,
                                                       int pitch) {
+  __shared__ Tile64 tile;
   const int i0 = blockIdx.x * 64, v0 = blockIdx.y * 64;
   transpose64(
+      tile,
       [&](int r, int c, float* v) {
         if (v0 + r < vocab) {
           ld8(w + static_cast<size_t>(v0 + r) * d + i0 + c, v);
