@@ -94,8 +94,9 @@ __device__ __forceinline__ double chunk_squares(const T* __restrict__ g, int n) 
   return v;
 }
 
+// o = g (pre c): pre is a power of two, so that c is a normal number however small the factor
 template <typename T>
-__device__ __forceinline__ void chunk_scale(const T* g, T* o, int n, float c) {
+__device__ __forceinline__ void chunk_scale(const T* g, T* o, int n, float pre, float c) {
   constexpr int N = Vec<T>::N;
   const int nv = ((reinterpret_cast<uintptr_t>(g) | reinterpret_cast<uintptr_t>(o)) & 15u) == 0 ? n / N : 0;
 #pragma unroll 4
@@ -104,16 +105,16 @@ __device__ __forceinline__ void chunk_scale(const T* g, T* o, int n, float c) {
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
       if constexpr (N == 4) {
-        v[k] = __float_as_uint(__uint_as_float(v[k]) * c);
+        v[k] = __float_as_uint(__uint_as_float(v[k]) * pre * c);
       } else {
-        const bf16_t lo = f32_to_bf16(__uint_as_float(v[k] << 16) * c);
-        const bf16_t hi = f32_to_bf16(__uint_as_float(v[k] & 0xffff0000u) * c);
+        const bf16_t lo = f32_to_bf16(__uint_as_float(v[k] << 16) * pre * c);
+        const bf16_t hi = f32_to_bf16(__uint_as_float(v[k] & 0xffff0000u) * pre * c);
         v[k] = static_cast<uint32_t>(lo) | (static_cast<uint32_t>(hi) << 16);
       }
     }
     __builtin_nontemporal_store(v, reinterpret_cast<u32x4*>(o + static_cast<size_t>(i) * N));
   }
-  for (int i = nv * N + threadIdx.x; i < n; i += 256) stf(o + i, ldf(g + i) * c);
+  for (int i = nv * N + threadIdx.x; i < n; i += 256) stf(o + i, ldf(g + i) * pre * c);
 }
 
 __global__ __launch_bounds__(256) void grad_norm_kernel(GradTable tab, double* __restrict__ part) {
@@ -145,14 +146,15 @@ __global__ __launch_bounds__(256) void grad_clip_kernel(GradTable tab, const dou
   const double v = norm_of(part, n);
   if (norm && blockIdx.x == 0 && threadIdx.x == 0) *norm = static_cast<float>(v);
   // a norm that is not a number makes every gradient one, an infinite one leaves zeros and NaN
-  const float c = v <= max_norm ? 1.0f : static_cast<float>(max_norm / v);
+  const double f = v <= max_norm ? 1.0 : max_norm / v;
+  const float pre = f < 0x1p-64 ? 0x1p-64f : 1.0f, c = static_cast<float>(f < 0x1p-64 ? f * 0x1p64 : f);
   // from the last chunk to the first: what the norm read last is still in the last-level cache
   for_chunks(tab, gridDim.x - 1 - blockIdx.x, [&](size_t at, int m, int i) {
-    if (c == 1.0f && tab.grad[i] == tab.out[i]) return;   // in place and unchanged
+    if (pre * c == 1.0f && tab.grad[i] == tab.out[i]) return;   // in place and unchanged
     if (tab.bf16[i])
-      chunk_scale(static_cast<const bf16_t*>(tab.grad[i]) + at, static_cast<bf16_t*>(tab.out[i]) + at, m, c);
+      chunk_scale(static_cast<const bf16_t*>(tab.grad[i]) + at, static_cast<bf16_t*>(tab.out[i]) + at, m, pre, c);
     else
-      chunk_scale(static_cast<const float*>(tab.grad[i]) + at, static_cast<float*>(tab.out[i]) + at, m, c);
+      chunk_scale(static_cast<const float*>(tab.grad[i]) + at, static_cast<float*>(tab.out[i]) + at, m, pre, c);
   });
 }
 

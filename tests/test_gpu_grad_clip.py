@@ -89,6 +89,12 @@ def test_squares_outside_the_range_of_fp32(lo, hi):
     Clip([(5000, "f32", 0), (5000, "bf16", 0)], 1e-3 if lo > 0 else 1e-33, False, lo=lo, hi=hi).run().check()
 
 
+def test_factor_below_the_normal_range():
+    """max_norm / norm of about 1e-42, which fp32 holds to three digits."""
+    print("case clip, a factor of 1e-42", flush=True)
+    Clip([(5000, "f32", 0), (5000, "bf16", 0), (5001, "f32", 1)], 1e-5, False, lo=35, hi=35).run().check()
+
+
 def test_zeros_and_values_that_are_not_finite():
     import torch
     print("case clip special values", flush=True)
