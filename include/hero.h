@@ -636,7 +636,8 @@ int hero_router_backward(const hero_dims *dims, int j, int T, const void *hbar, 
  * ------------------------------------------------------------------------------------- */
 
 /* The model's final norm, x = RMSNorm(h) * norm_w per token row; h, x [T][d], norm_w [d] in dims.dtype, eps
- * dims.eps_norm.  x must not overlap h or norm_w.  d <= 32768 (HERO_E_UNSUPPORTED above). */
+ * dims.eps_norm.  x must not overlap h or norm_w.  d <= 32768, T <= 4194240 (HERO_E_UNSUPPORTED above; also of its
+ * backward). */
 int hero_final_norm(const hero_dims *dims, int T, const void *h, const void *norm_w, void *x, void *stream);
 
 /*
@@ -692,9 +693,10 @@ int hero_lm_loss_workspace_size(const hero_dims *dims, int vocab, int T, int wit
  * The vocabulary is taken in pieces whose exponentials live in the workspace.  Products are bf16 x bf16 with
  * fp32 accumulation for a bf16 model, where exp(logit - reference) passes through memory in bf16 on its way to
  * dx, and p - [v = y] to dw (fp32 otherwise); losses, sums and the target's own share are fp32 throughout.  A
- * logit that is not finite leaves no finite loss or gradient of its token.
+ * logit of NaN or +infinity, and a target's of -infinity, leave no finite loss or gradient of their token; any other
+ * of -infinity has no share in the loss.  fp32 models: elements of x and w above 3.38e38 count as infinite.
  * Every sum runs in a fixed order.
- * Errors: HERO_E_DIM (vocab, T), HERO_E_UNSUPPORTED (vocab above 4194240, T above 2^24; bf16: vocab below 65, or
+ * Errors: HERO_E_DIM (vocab, T), HERO_E_UNSUPPORTED (vocab or T above 4194240; bf16: vocab below 65, or
  * x, w_t, or 131072 rows of w spanning 4 GiB or more), HERO_E_RANGE (reduction, scale not finite), HERO_E_NULL (w_t with dx),
  * HERO_E_ALIGN, HERO_E_ALIAS, HERO_E_WORKSPACE, HERO_E_DEVICE, HERO_E_LAUNCH.
  */
@@ -727,7 +729,7 @@ int hero_grad_norm(int n_tensors, const hero_grad_tensor *tensors, float *norm, 
 /*
  * norm[0] as above, and out = grad * min(1, max_norm / norm) in each tensor's dtype, rounded once.  max_norm >= 0
  * (HERO_E_RANGE; +inf is allowed).  Where the factor is 1, a tensor scaled in place is not touched.  A norm that is
- * NaN makes every element NaN, an infinite one zero or NaN.  The list travels with the launches: nothing of it is read
+ * NaN makes every element NaN, an infinite one zero or NaN (max_norm of +inf: nothing is scaled).  The list travels with the launches: nothing of it is read
  * after the call returns, and a captured call replays with the same pointers.
  */
 int hero_grad_clip(int n_tensors, const hero_grad_tensor *tensors, float max_norm, float *norm, void *workspace,

@@ -1708,7 +1708,7 @@ constexpr int kLmChunk = 8192;               // rows of one chunk
 // 256, 512 MiB and 1 GiB 12.97, 12.47, 12.31 and 12.21 ms, 2048 counted tokens 3.34, 3.23, 3.14 and 3.11.
 constexpr size_t kLmPiece = 256u << 20;
 constexpr size_t kLmTerms = 128u << 20;      // elements of a piece's head rows in three terms
-constexpr int kLmVocabMax = 65535 * 64;      // grid limit of the head's transpose
+constexpr int kEndsMost = 65535 * 64;        // vocabulary and tokens: the grids' second axis in transposes, 64 a workgroup
 constexpr int kLmVocabMin = 65;              // matrix cores: the products take K in at least two k-tiles
 constexpr int kLmHeadRows = 1 << 17;         // head rows of a product, which addresses them with 32 bits
 
@@ -1825,7 +1825,7 @@ int check_lm(const hero_dims* dims, int vocab, int T, bool dx, bool dw) {
   const int st = check_dims(dims);
   if (st != HERO_OK) return st;
   if (vocab <= 0 || T <= 0) return HERO_E_DIM;
-  if (vocab > kLmVocabMax || T > (1 << 24)) return HERO_E_UNSUPPORTED;
+  if (vocab > kEndsMost || T > kEndsMost) return HERO_E_UNSUPPORTED;
   if (dims->dtype != HERO_BF16) return HERO_OK;
   const long long d = dims->d;
   if (vocab < kLmVocabMin || T * d * 2 >= kGemmSpan || 256 * d * 2 >= kGemmSpan) return HERO_E_UNSUPPORTED;
@@ -1841,7 +1841,7 @@ int hero_final_norm(const hero_dims* dims, int T, const void* h, const void* nor
   int st = check_dims(dims);
   if (st != HERO_OK) return st;
   if (T <= 0) return HERO_E_DIM;
-  if (dims->d > hero::kNormWidest) return HERO_E_UNSUPPORTED;
+  if (dims->d > hero::kNormWidest || T > kEndsMost) return HERO_E_UNSUPPORTED;
   if (!h || !norm_w || !x) return HERO_E_NULL;
   if (!aligned16(h) || !aligned16(norm_w) || !aligned16(x)) return HERO_E_ALIGN;
   const size_t wb = static_cast<size_t>(dims->d) * esize(dims->dtype), hb = wb * T;
@@ -1860,7 +1860,7 @@ int hero_final_norm_backward_workspace_size(const hero_dims* dims, int T, size_t
   const int st = check_dims(dims);
   if (st != HERO_OK) return st;
   if (T <= 0) return HERO_E_DIM;
-  if (dims->d > hero::kNormWidest) return HERO_E_UNSUPPORTED;
+  if (dims->d > hero::kNormWidest || T > kEndsMost) return HERO_E_UNSUPPORTED;
   *bytes = align_up(static_cast<size_t>(hero::final_norm_bwd_groups(T, dims->d)) * dims->d * 4);
   return HERO_OK;
 }

@@ -243,6 +243,27 @@ def test_two_calls_on_two_streams():
     _check(cb, b[2])
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("T,V", [(5, 1000), (5, 9001), (200, 1000), (300, 40001)])
+def test_logits_of_minus_infinity(T, V, dtype):
+    """A head row whose logits are below the range: no share in a loss, zeros in dW, and dx as without it."""
+    from tests import train_ends as E
+    print(f"case lm_loss -inf T={T} V={V} {dtype}", flush=True)
+    x, w, y = _inputs(T, 256, V, dtype, 21, sure=0.0)
+    x.abs_()
+    y[y == 7] = 8
+    w[7] = -3e38
+    assert x.double().sum(1).min() > 10          # times 3e38: past the range of fp32
+    got = E.Loss(x, w, y).run().results()
+    assert not got["dw"][7].any()
+    w[7] = -100.0                                 # logits of -1000 and less: exponentials of zero in 64 bits too
+    x64, w64 = E.f64(x), E.f64(w)
+    c = E.Loss(x, w, y)
+    # the row without size: its exp(0) of a sum of V others of about e takes less than 1 in 100 of what they are bounded by
+    bounds = E.loss_bounds(x64, np.where(np.arange(V)[:, None] == 7, 0.0, w64), y, 1.0, True, dtype)
+    E.check_loss(c, O.lm_loss(x64, w64, y), [1.01 * b for b in bounds], got)
+
+
 @pytest.mark.parametrize("T,dtype", [(5, "bf16"), (300, "bf16"), (70, "f32"), (1200, "f32"), (1100, "bf16")])
 def test_graph_replays_with_new_inputs(T, dtype):
     """Targets, and with them the number of rows, change between the replays; eager work runs in between."""

@@ -104,6 +104,16 @@ def test_final_norm_backward_refusals(change, status):
                                       None) == status
 
 
+def test_most_tokens():
+    """The limit on the tokens, where the spans of the arrays allow more."""
+    most, f32 = 4194240, good_dims(H.HERO_F32)
+    assert loss(dims=good_dims(d=256), T=most + 1) == loss(dims=f32, T=most + 1) == H.HERO_E_UNSUPPORTED
+    assert size("hero_lm_loss_workspace_size", ctypes.byref(f32), V, most, 1, 1)[0] == H.HERO_OK
+    assert size("hero_lm_loss_workspace_size", ctypes.byref(good_dims(d=256)), V, most, 1, 1)[0] == H.HERO_OK
+    assert size("hero_final_norm_backward_workspace_size", ctypes.byref(f32), most + 1)[0] == H.HERO_E_UNSUPPORTED
+    assert H.hero_final_norm(f32, most + 1, at(1), at(2), at(3), None) == H.HERO_E_UNSUPPORTED
+
+
 F, B = H.HERO_F32, H.HERO_BF16
 
 
