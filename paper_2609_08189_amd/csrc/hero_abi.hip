@@ -1723,10 +1723,11 @@ struct LmLayout {
   int chunk, n_chunks;       // rows of a chunk, chunks of T rows
   int cols, pieces, pitch;   // columns of a piece (the last takes the rest), widest piece's pitch
   int ldl;                   // pitch of kept logits
-  int slices;                // most K slices of them, 0: none kept
+  int slices;                // most K slices of them (kLmF32: 1 where e is, in their place), 0: none kept
   bool single;               // one piece and one chunk: dW is formed from e
   bool keep_e;
   int acc_rows, dx_depth, f32_slices;
+  bool f32_few;
   int g_cols, g_pitch, g_ldl;
   int dw_slices;
   size_t idx, inv, tgt, counts, plan, done, lt, ref, sum, alpha, nll, lse, own, e, part, acc, g, xT, logits, xs, ws, wts,
@@ -1754,13 +1755,21 @@ LmLayout lm_layout_of(const hero_dims& d, int vocab, int T, bool dx, bool dw) {
   auto fit = [&](size_t rows) {
     size_t c = kLmPiece / rows;
     if (split) c = std::min(c, kLmTerms / w);
-    const size_t most = std::min<size_t>((static_cast<size_t>(vocab) + 255) / 256 * 256, kLmHeadRows - 256);
+    const size_t most = std::min<size_t>((static_cast<size_t>(vocab) + 255) / 256 * 256, kLmHeadRows);
     return static_cast<int>(std::min(std::max<size_t>(c / 256 * 256, 256), most));
   };
   L.chunk = std::min(T, kLmChunk);
   L.n_chunks = (T + L.chunk - 1) / L.chunk;
   L.cols = fit(static_cast<size_t>(L.chunk));
-  L.pieces = std::max(1, (vocab - 127 + L.cols - 1) / L.cols);   // no piece of less than two k-tiles
+  // Whole pieces and a rest, which fill rounds of workgroups best, but pieces of one width where the rest would be less
+  // than a quarter: it would leave all of them its few K slices, and its own launches few workgroups (96 rows against
+  // 131072 columns, 256 of them the rest: 1840 -> 418 us; half of 8192 against 70000 2525 -> 2351).
+  const auto even = [&](int cols, int n) {
+    return n > 1 && vocab - (n - 1) * cols < cols / 4 ? std::min(cols, up((vocab + n - 1) / n, 256)) : cols;
+  };
+  const auto pieces = [&] { return std::max(1, (vocab - 127 + L.cols - 1) / L.cols); };   // none of less than two k-tiles
+  L.cols = even(L.cols, pieces());
+  L.pieces = pieces();
   const int last = vocab - (L.pieces - 1) * L.cols, widest = L.pieces > 1 ? std::max(L.cols, last) : last;
   const int narrowest = L.pieces > 1 ? std::min(L.cols, last) : last;
   L.pitch = up(widest, 64);
@@ -1769,11 +1778,13 @@ LmLayout lm_layout_of(const hero_dims& d, int vocab, int T, bool dx, bool dw) {
   // what the logits of every piece's width need (kLmF32: the logits are e's buffer)
   const hero::LmParts pw = hero::lm_parts(L.mode, L.chunk, L.cols, d.d), pl = hero::lm_parts(L.mode, L.chunk, last, d.d);
   const bool many = L.pieces > 1;
-  L.slices = std::max(many ? pw.slices : 0, pl.slices);
+  L.slices = std::max({many ? pw.slices : 0, pl.slices, mfma ? 0 : static_cast<int>(L.keep_e)});
   const int parts = std::max(many ? pw.parts : 0, pl.parts);
   L.ldl = mfma ? up(widest, 256) : L.pitch;
   L.dx_depth = up(narrowest, 64) / 64 * (split ? 6 : 1);
-  L.f32_slices = mfma ? 1 : hero::lm_f32_slices(L.chunk, d.d, up(narrowest, 64));
+  const int few_slices = mfma ? 0 : hero::lm_f32_few_slices(L.chunk, d.d, up(narrowest, 64));
+  L.f32_few = few_slices > 0;
+  L.f32_slices = mfma ? 1 : L.f32_few ? few_slices : hero::lm_f32_slices(L.chunk, d.d, up(narrowest, 64));
   const size_t c = static_cast<size_t>(L.chunk);
   // rows of the accumulators' K slices: up to 256 MiB of them
   L.acc_rows = !dx ? 0 : mfma ? static_cast<int>(std::max(c, std::min(c * hero::kLmDxSlices, (64u << 20) / w)))
@@ -1793,7 +1804,8 @@ LmLayout lm_layout_of(const hero_dims& d, int vocab, int T, bool dx, bool dw) {
   L.own = take(t * 4);
   const bool few = L.single && hero::lm_dw_few_rows(L.mode, T);   // no two k-tiles there, but in bf16 two terms of g
   L.g_pitch = mfma && !few ? std::max(128, up(T, 64)) : up(T, 64);
-  L.g_cols = L.single ? vocab : fit(static_cast<size_t>(L.g_pitch));
+  L.g_cols = fit(static_cast<size_t>(L.g_pitch));
+  L.g_cols = L.single ? vocab : even(L.g_cols, (vocab + L.g_cols - 1) / L.g_cols);
   L.g_ldl = up(std::min(L.g_cols, vocab), 64);
   // of several pieces or chunks, e is done with when g is formed (kLmF32: e is the logits')
   const size_t gb = dw ? static_cast<size_t>(std::min(L.g_cols, vocab)) * L.g_pitch * (few && mfma ? 2 * es : es) : 0;
@@ -1970,6 +1982,7 @@ int hero_lm_loss(const hero_dims* dims, int vocab, int T, const void* x, const h
   a.dx_depth = L.dx_depth;
   a.acc_rows = L.acc_rows;
   a.f32_slices = L.f32_slices;
+  a.f32_few = L.f32_few;
   a.xs = ws + L.xs;
   const bool mfma = L.mode != hero::kLmF32, split = L.mode == hero::kLmSplit;
   const float* wf = static_cast<const float*>(head->w);

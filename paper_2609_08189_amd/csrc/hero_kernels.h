@@ -432,6 +432,7 @@ struct LmRows {
   // chunks of rows, and what the dx products' plan goes by: column tiles, k-tiles, rows of the accumulators
   int chunk, n_chunks, dx_tiles, dx_depth, acc_rows;
   int f32_slices;            // kLmF32: K slices
+  bool f32_few;              // ... of the streaming dx product
   void* xs;                  // kLmSplit: [3][T][d] the rows' terms
 };
 // the rows, their targets' logits; everything else that a call starts from
@@ -457,6 +458,8 @@ struct LmPiece {
 constexpr int kLmLogitsMax = 8192;   // columns of a piece whose logits are kept (kLmF32: of any)
 constexpr int kLmFewRows = 64;       // bf16 rows that the head streams past at once,
 constexpr long long kLmFewHead = 80000000;   // and elements of such a head
+constexpr int kLmFewF32 = 112;       // fp32 rows do so from so many columns in 128s on,
+constexpr long long kLmFewDx = 12000000;     // and W^T past the rows of e from so many elements
 // which of the forms the logits take: parts and shift of a row (slices 0), or K slices of kept logits
 struct LmParts {
   int parts, shift, slices;
@@ -475,6 +478,7 @@ hipError_t launch_lm_f32_dx(const float* e, const int* count, int rows_max, int 
                             int slices, const float* alpha, bool first, float* acc, hipStream_t s);
 hipError_t launch_lm_f32_dw(const float* g, int cols, const float* xT, int d, int pitch, float* dw, hipStream_t s);
 int lm_f32_slices(int rows, int d, int K);
+int lm_f32_few_slices(int rows, int d, int K);   // k_lm_gemm.hip
 
 // dW of the columns [v0, v0 + cols), all rows at once.  g [cols][pitch]: p - [target] (kLmF32: times the
 // unit, scale / N), the rows contiguous, zero behind the last; xT [d][pitch]: the counted rows of x,

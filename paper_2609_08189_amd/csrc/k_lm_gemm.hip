@@ -331,73 +331,103 @@ __global__ __launch_bounds__(256) void lm_dw_few(LmRows a, int cols, const T* __
 // under way: on the large products' tiles, of which small heads have too few, two k-tiles of 125 CUs drew 2.9 TB/s.
 // Operand A: 32 head rows a wave, B: the rows of x.  One barrier a k-tile: past it every wave has the tile's loads of
 // all waves, and none reads the tile before any more, whose place the next loads take.
+// fp32: a k-tile's 128 bytes of a row are 32 elements, and a lane's 16 bytes feed four matrix instructions.
 // ---------------------------------------------------------------------------
-template <int TB, int NS, bool STORE>
-__global__ __launch_bounds__(256) void lm_logits_few(LmRows a, LmPiece p) {
-  constexpr int BV = 128, BX = 16 * TB, STAGE = (BV + BX) * ROWB;
-  constexpr int XL = TB < 4 ? 1 : 2;               // loads a wave of x (TB 1: two waves repeat the others')
-  constexpr int L = 4 + XL;
-  __shared__ __attribute__((aligned(1024))) unsigned char smem[NS * STAGE];
-  const int M = *p.count;
-  if (M == 0) return;
-  const int lane = threadIdx.x & 63, l15 = lane & 15, q = lane >> 4, rsub = lane >> 3;
-  const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) >> 6);
-  const int v0 = blockIdx.x * BV;
-  const unsigned char* w = reinterpret_cast<const unsigned char*>(static_cast<const bf16_t*>(a.w) + static_cast<size_t>(p.v0) * a.d);
-  const unsigned char* x = static_cast<const unsigned char*>(a.x);
-  uint32_t w_off[4], x_off[XL];
+template <typename T, int TB, int NS>
+struct FewRing {
+  static constexpr bool F32 = std::is_same_v<T, float>;
+  static constexpr int BV = 128, BX = 16 * TB, STAGE = (BV + BX) * ROWB;
+  static constexpr int XL = TB < 4 ? 1 : 2;        // loads a wave of x (TB 1: two waves repeat the others')
+  static constexpr int L = 4 + XL;
+  typedef std::conditional_t<F32, f32x4, bf16x8> Frag;
+  // acc[f][b]: rows 16 f of the wave's 32 of w (`rows` of them, the last repeated), rows 16 b of x; w and x at k-tile 0 of
+  // nkt >= NS - 1, x_row(r) the byte offset of row r
+  template <class X>
+  static __device__ __forceinline__ void run(const unsigned char* w, size_t w_bytes, int rows, const unsigned char* x, X x_row,
+                                             int nkt, unsigned char* smem, f32x4 (&acc)[2][TB]) {
+    const int lane = threadIdx.x & 63, l15 = lane & 15, rsub = lane >> 3;
+    const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) >> 6);
+    uint32_t w_off[4], x_off[XL];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int r = 8 * (4 * i + wave) + rsub, ch = (lane & 7) ^ ((r >> 1) & 7);
-    w_off[i] = static_cast<uint32_t>(min(v0 + r, p.cols - 1)) * static_cast<uint32_t>(a.d * 2) + ch * 16;
-  }
-  const auto x_block = [&](int i) { return (4 * i + wave) % (2 * TB); };   // of eight rows
+    for (int i = 0; i < 4; ++i) {
+      const int r = 8 * (4 * i + wave) + rsub, ch = (lane & 7) ^ ((r >> 1) & 7);
+      w_off[i] = static_cast<uint32_t>(min(r, rows - 1)) * static_cast<uint32_t>(w_bytes) + ch * 16;
+    }
+    const auto x_block = [&](int i) { return (4 * i + wave) % (2 * TB); };   // of eight rows
 #pragma unroll
-  for (int i = 0; i < XL; ++i) {
-    const int r = 8 * x_block(i) + rsub, ch = (lane & 7) ^ ((r >> 1) & 7);
-    x_off[i] = static_cast<uint32_t>(a.idx[p.m0 + min(r, M - 1)]) * static_cast<uint32_t>(a.d * 2) + ch * 16;
-  }
-  const int nkt = a.d / BK;
-  auto issue = [&](int kt) {
-    unsigned char* st = smem + kt % NS * STAGE;
-    const uint32_t kb = static_cast<uint32_t>(kt) * ROWB;
+    for (int i = 0; i < XL; ++i) {
+      const int r = 8 * x_block(i) + rsub, ch = (lane & 7) ^ ((r >> 1) & 7);
+      x_off[i] = x_row(r) + ch * 16;
+    }
+    auto issue = [&](int kt) {
+      unsigned char* st = smem + kt % NS * STAGE;
+      const uint32_t kb = static_cast<uint32_t>(kt) * ROWB;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) load_lds16(w + kb + w_off[i], st + (4 * i + wave) * 1024);
+      for (int i = 0; i < 4; ++i) load_lds16(w + kb + w_off[i], st + (4 * i + wave) * 1024);
 #pragma unroll
-    for (int i = 0; i < XL; ++i) load_lds16(x + kb + x_off[i], st + BV * ROWB + x_block(i) * 1024);
-  };
-  f32x4 acc[2][TB];
+      for (int i = 0; i < XL; ++i) load_lds16(x + kb + x_off[i], st + BV * ROWB + x_block(i) * 1024);
+    };
 #pragma unroll
-  for (int f = 0; f < 2; ++f)
+    for (int f = 0; f < 2; ++f)
 #pragma unroll
-    for (int b = 0; b < TB; ++b) acc[f][b] = f32x4{0.f, 0.f, 0.f, 0.f};
+      for (int b = 0; b < TB; ++b) acc[f][b] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-  for (int k = 0; k < NS - 1; ++k) issue(k);       // d >= 256: four k-tiles at least
-  static_assert(NS <= 5, "the first loads are of tiles that exist");
-  for (int kt = 0; kt < nkt; ++kt) {
-    // this wave's loads of tile kt have landed (NS - 2 tiles behind it may be in flight; near the end all have)
-    if (kt + NS - 1 <= nkt)
-      wait_vm_lgkm<(NS - 2) * L>();
-    else
-      wait_vm_lgkm<0>();
-    __builtin_amdgcn_s_barrier();
-    __builtin_amdgcn_sched_barrier(0);
-    if (kt + NS - 1 < nkt) issue(kt + NS - 1);
-    const unsigned char* st = smem + kt % NS * STAGE;
+    for (int k = 0; k < NS - 1; ++k) issue(k);
+    for (int kt = 0; kt < nkt; ++kt) {
+      // this wave's loads of tile kt have landed (NS - 2 tiles behind it may be in flight; near the end all have)
+      if (kt + NS - 1 <= nkt)
+        wait_vm_lgkm<(NS - 2) * L>();
+      else
+        wait_vm_lgkm<0>();
+      __builtin_amdgcn_s_barrier();
+      __builtin_amdgcn_sched_barrier(0);
+      if (kt + NS - 1 < nkt) issue(kt + NS - 1);
+      const unsigned char* st = smem + kt % NS * STAGE;
 #pragma unroll
-    for (int ks = 0; ks < 2; ++ks) {
-      const int c = in_chunk<16>(ks, lane);
-      bf16x8 fw[2], fx[TB];
+      for (int ks = 0; ks < 2; ++ks) {
+        const int c = in_chunk<16>(ks, lane);
+        Frag fw[2], fx[TB];
 #pragma unroll
-      for (int f = 0; f < 2; ++f) fw[f] = *reinterpret_cast<const bf16x8*>(st + swz(wave * 32 + 16 * f + l15, c));
+        for (int f = 0; f < 2; ++f) fw[f] = *reinterpret_cast<const Frag*>(st + swz(wave * 32 + 16 * f + l15, c));
 #pragma unroll
-      for (int b = 0; b < TB; ++b) fx[b] = *reinterpret_cast<const bf16x8*>(st + BV * ROWB + swz(16 * b + l15, c));
+        for (int b = 0; b < TB; ++b) fx[b] = *reinterpret_cast<const Frag*>(st + BV * ROWB + swz(16 * b + l15, c));
+        if constexpr (F32) {
 #pragma unroll
-      for (int f = 0; f < 2; ++f)
+          for (int e = 0; e < 4; ++e)
 #pragma unroll
-        for (int b = 0; b < TB; ++b) acc[f][b] = mfma_op(fw[f], fx[b], acc[f][b]);
+            for (int f = 0; f < 2; ++f)
+#pragma unroll
+              for (int b = 0; b < TB; ++b)
+                acc[f][b] = __builtin_amdgcn_mfma_f32_16x16x4f32(fw[f][e], fx[b][e], acc[f][b], 0, 0, 0);
+        } else {
+#pragma unroll
+          for (int f = 0; f < 2; ++f)
+#pragma unroll
+            for (int b = 0; b < TB; ++b) acc[f][b] = mfma_op(fw[f], fx[b], acc[f][b]);
+        }
+      }
     }
   }
+};
+
+template <typename T, int TB, int NS, bool STORE>
+__global__ __launch_bounds__(256) void lm_logits_few(LmRows a, LmPiece p) {
+  typedef FewRing<T, TB, NS> R;
+  constexpr bool F32 = R::F32;
+  constexpr int BX = R::BX;
+  __shared__ __attribute__((aligned(1024))) unsigned char smem[NS * R::STAGE];
+  const int M = *p.count;
+  if (M == 0) return;
+  const int lane = threadIdx.x & 63, l15 = lane & 15, q = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) >> 6);
+  const int v0 = blockIdx.x * R::BV;
+  const size_t row_bytes = static_cast<size_t>(a.d) * sizeof(T);
+  f32x4 acc[2][TB];
+  R::run(static_cast<const unsigned char*>(a.w) + static_cast<size_t>(p.v0 + v0) * row_bytes, row_bytes, p.cols - v0,
+         static_cast<const unsigned char*>(a.x),
+         [&](int r) { return static_cast<uint32_t>(a.idx[p.m0 + min(r, M - 1)]) * static_cast<uint32_t>(row_bytes); },
+         static_cast<int>(row_bytes / ROWB), smem, acc);   // d >= 256, fp32 128: four k-tiles at least
+  static_assert(NS <= 5, "the first loads are of tiles that exist");
   // every wave is past its last reads; the ring's memory holds the columns' maxima and sums now
   asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
   __syncthreads();
@@ -428,18 +458,22 @@ __global__ __launch_bounds__(256) void lm_logits_few(LmRows a, LmPiece p) {
     float s = 0.f;
 #pragma unroll
     for (int f = 0; f < 2; ++f) {
-      uint32_t o[2];
+      float o[4];
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
         const int k = 16 * f + r;
-        const float v = n0 + k < p.cols && k != tgt ? __expf(acc[f][b][r] - ref[b]) : 0.f;
-        s += v;
-        const uint32_t h = f32_to_bf16(v);
-        o[r >> 1] = r & 1 ? o[r >> 1] | h << 16 : h;
+        o[r] = n0 + k < p.cols && k != tgt ? lm_exp<F32>(acc[f][b][r] - ref[b]) : 0.f;
+        s += o[r];
       }
       if constexpr (STORE)
-        if (m < M && n0 + 16 * f < p.pitch)
-          *reinterpret_cast<uint2*>(static_cast<bf16_t*>(p.e) + static_cast<size_t>(m) * p.pitch + n0 + 16 * f) = uint2{o[0], o[1]};
+        if (m < M && n0 + 16 * f < p.pitch) {
+          T* e = static_cast<T*>(p.e) + static_cast<size_t>(m) * p.pitch + n0 + 16 * f;
+          if constexpr (F32)
+            *reinterpret_cast<f32x4*>(e) = f32x4{o[0], o[1], o[2], o[3]};
+          else
+            *reinterpret_cast<uint2*>(e) = uint2{f32_to_bf16(o[0]) | static_cast<uint32_t>(f32_to_bf16(o[1])) << 16,
+                                                 f32_to_bf16(o[2]) | static_cast<uint32_t>(f32_to_bf16(o[3])) << 16};
+        }
     }
     s += __shfl_xor(s, 16, kWave);
     s += __shfl_xor(s, 32, kWave);
@@ -454,6 +488,34 @@ __global__ __launch_bounds__(256) void lm_logits_few(LmRows a, LmPiece p) {
         p.part[static_cast<size_t>(m) * p.parts + blockIdx.x] = {
             ref[b], (sums[m] + sums[BX + m]) + (sums[2 * BX + m] + sums[3 * BX + m])};
     }
+}
+
+// dx of few fp32 rows the same way: W^T streams past the rows of e, slice z of K into acc + z M d
+template <int TB, int NS>
+__global__ __launch_bounds__(256) void lm_f32_dx_few(LmRows a, LmPiece p, const float* __restrict__ w_t, int ld_wt, int slices) {
+  typedef FewRing<float, TB, NS> R;
+  __shared__ __attribute__((aligned(1024))) unsigned char smem[NS * R::STAGE];
+  const int M = *p.count;
+  if (M == 0) return;
+  const int lane = threadIdx.x & 63, l15 = lane & 15, q = lane >> 4, wave = threadIdx.x >> 6;
+  const int i0 = blockIdx.x * R::BV, z = blockIdx.y, all = p.pitch * 4 / ROWB;
+  const int k0 = static_cast<int>(static_cast<long long>(all) * z / slices);
+  const int nkt = static_cast<int>(static_cast<long long>(all) * (z + 1) / slices) - k0;
+  f32x4 acc[2][TB];
+  R::run(reinterpret_cast<const unsigned char*>(w_t + static_cast<size_t>(i0) * ld_wt + p.v0) + static_cast<size_t>(k0) * ROWB,
+         static_cast<size_t>(ld_wt) * 4, a.d - i0, static_cast<const unsigned char*>(p.e) + static_cast<size_t>(k0) * ROWB,
+         [&](int r) { return static_cast<uint32_t>(min(r, M - 1)) * static_cast<uint32_t>(p.pitch * 4); }, nkt, smem, acc);
+  float* out = p.acc + static_cast<size_t>(z) * M * a.d + i0 + wave * 32 + 4 * q;   // lane: columns 16 f + r of row 16 b + l15
+#pragma unroll
+  for (int b = 0; b < TB; ++b) {
+    const int m = 16 * b + l15;
+    if (m >= M) continue;
+#pragma unroll
+    for (int f = 0; f < 2; ++f) {
+      f32x4* o = reinterpret_cast<f32x4*>(out + static_cast<size_t>(m) * a.d + 16 * f);
+      *o = p.first ? acc[f][b] : a.alpha[p.m0 + m] * *o + acc[f][b];
+    }
+  }
 }
 
 int lm_tiles(int n) { return (n + 255) / 256; }
@@ -536,28 +598,41 @@ hipError_t lm_dw(const LmRows& a, int v0, int cols, const void* g, const void* x
 // 160 MB: the streaming form (3 rows of d = 768 against 77287 columns 43 -> 34 us a call, 8 of 2048 against 9000
 // 48 -> 37); larger heads draw 5.6 TB/s on the large tiles and 4.8 there (16 rows of 4096 against 128256: 185 and 222 us).
 // Longer rows gain nothing from slices:
-// 10 rows of d = 2048 against 39058 columns, 153 tiles, took 56 us so and 65 + 7 in five slices.  kLmF32: always kept.
+// 10 rows of d = 2048 against 39058 columns, 153 tiles, took 56 us so and 65 + 7 in five slices.  kLmF32: kept, or for few
+// rows the streaming form (28 rows of d = 3840 against 75583 columns 462 -> 256 us a call, 4.6 TB/s; 60 of 1024 against
+// 30000 82 -> 54) where its workgroups take most CUs (64 of them: one row of 4096 against 8192 45 -> 67).
 LmParts lm_parts(int mode, int rows, int cols, int d) {
-  if (mode == kLmF32) return cols <= kLmLogitsMax ? LmParts{0, 0, 1} : LmParts{(cols + 8191) / 8192, 13, 1};
+  const LmParts few{(cols + 127) / 128, 7, 0};
+  if (mode == kLmF32) {
+    if (rows <= kLmFewRows && (cols + 127) / 128 >= kLmFewF32) return few;
+    return cols <= kLmLogitsMax ? LmParts{0, 0, 1} : LmParts{(cols + 8191) / 8192, 13, 1};
+  }
   const int tiles = (rows + 127) / 128 * lm_tiles(cols), ktiles = d / 64 * (mode == kLmSplit ? 6 : 1);
   const int S = 2 * tiles > kCUs || cols > kLmLogitsMax - 256 ? 1 : std::min(kCUs / tiles, ktiles / 4);
   if (S > 1) return {0, 0, S};
-  if (mode == kLmBf16 && rows <= kLmFewRows && static_cast<long long>(cols) * d <= kLmFewHead) return {(cols + 127) / 128, 7, 0};
+  if (mode == kLmBf16 && rows <= kLmFewRows && static_cast<long long>(cols) * d <= kLmFewHead) return few;
   return {4 * lm_tiles(cols), 0, 0};
 }
 
 hipError_t launch_lm_logits(const LmRows& a, const LmPiece& p, hipStream_t s) {
-  if (a.mode == kLmBf16 && p.shift) {   // the streaming form
+  if (!p.logits && p.shift) {   // the streaming form
     const int grid = (p.cols + 127) / 128;
-#define HERO_LM_FEW(TB, NS)                                      \
-  (p.e ? lm_logits_few<TB, NS, true><<<grid, 256, 0, s>>>(a, p) \
-       : lm_logits_few<TB, NS, false><<<grid, 256, 0, s>>>(a, p))
-    if (p.rows_max <= 16)
-      HERO_LM_FEW(1, 4);
-    else if (p.rows_max <= 32)
-      HERO_LM_FEW(2, 4);
-    else
-      HERO_LM_FEW(4, 3);
+#define HERO_LM_FEW(T, TB, NS)                                      \
+  (p.e ? lm_logits_few<T, TB, NS, true><<<grid, 256, 0, s>>>(a, p) \
+       : lm_logits_few<T, TB, NS, false><<<grid, 256, 0, s>>>(a, p))
+#define HERO_LM_FEW_ROWS(T)      \
+  if (p.rows_max <= 16)          \
+    HERO_LM_FEW(T, 1, 4);        \
+  else if (p.rows_max <= 32)     \
+    HERO_LM_FEW(T, 2, 4);        \
+  else                           \
+    HERO_LM_FEW(T, 4, 3)
+    if (a.mode == kLmBf16) {
+      HERO_LM_FEW_ROWS(bf16_t);
+    } else {
+      HERO_LM_FEW_ROWS(float);
+    }
+#undef HERO_LM_FEW_ROWS
 #undef HERO_LM_FEW
     return hipGetLastError();
   }
@@ -567,9 +642,28 @@ hipError_t launch_lm_logits(const LmRows& a, const LmPiece& p, hipStream_t s) {
                               static_cast<const float*>(a.w) + static_cast<size_t>(p.v0) * a.d, p.cols, a.d, p.logits, p.ldl, s);
 }
 
+// K slices of the streaming dx product, of at least 256 columns each: two workgroups a CU; 0: the other form, whose tiles
+// read 64-byte pieces of rows (60 rows of d = 4096 against 128256 columns with the logits 1759 -> 1175 us a call, 60 of 256
+// against 100000 176 -> 130; against 10000 of d = 1024 80 and 83)
+int lm_f32_few_slices(int rows, int d, int K) {
+  if (rows > kLmFewRows || K < 256 || static_cast<long long>(d) * K < kLmFewDx) return 0;
+  return std::max(1, std::min({2 * kCUs / (d / 128), K / 256, 64}));
+}
+
 hipError_t launch_lm_dx(const LmRows& a, const LmPiece& p, const void* w_t, int ld_wt, hipStream_t s) {
   if (a.mode == kLmBf16) return lm_dx<false>(a, p, w_t, ld_wt, s);
   if (a.mode == kLmSplit) return lm_dx<true>(a, p, nullptr, 0, s);
+  if (a.f32_few) {
+    const float* wt = static_cast<const float*>(w_t);
+    const dim3 grid(a.d / 128, a.f32_slices);
+    if (p.rows_max <= 16)
+      lm_f32_dx_few<1, 4><<<grid, 256, 0, s>>>(a, p, wt, ld_wt, a.f32_slices);
+    else if (p.rows_max <= 32)
+      lm_f32_dx_few<2, 4><<<grid, 256, 0, s>>>(a, p, wt, ld_wt, a.f32_slices);
+    else
+      lm_f32_dx_few<4, 3><<<grid, 256, 0, s>>>(a, p, wt, ld_wt, a.f32_slices);
+    return hipGetLastError();
+  }
   return launch_lm_f32_dx(static_cast<const float*>(p.e), p.count, p.rows_max, p.pitch, static_cast<const float*>(w_t) + p.v0,
                           ld_wt, a.d, a.f32_slices, a.alpha + p.m0, p.first, p.acc, s);
 }

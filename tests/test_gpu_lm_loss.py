@@ -243,6 +243,24 @@ def test_two_calls_on_two_streams():
     _check(cb, b[2])
 
 
+@pytest.mark.parametrize("T,d,V,size", [(1, 512, 30000, 1.0), (16, 1024, 15001, 1.0), (17, 640, 33003, 1.0), (33, 512, 30001, 1.0),
+                                        (64, 1024, 16000, 1.0), (20, 512, 30000, 120.0), (50, 256, 140001, 60.0), (3, 128, 131073, 1.0)])
+def test_few_fp32_rows_against_large_heads(T, d, V, size):
+    from tests import train_ends as E
+    print(f"case lm_loss few fp32 rows T={T} d={d} V={V} size={size}", flush=True)
+    x, w, y = _inputs(T, d, V, "f32", T + V, keep=1.0 if T < 4 else 0.9, size=size, sure=2.0)
+    _check(E.Loss(x, w, y, mean=False).run(), y)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("T,V", [(90, 131072), (90, 131073), (90, 131199), (90, 131200), (3, 262150), (8192, 33000)])
+def test_last_pieces_that_would_be_narrow(T, V, dtype):
+    from tests import train_ends as E
+    print(f"case lm_loss narrow rest T={T} V={V} {dtype}", flush=True)
+    x, w, y = _inputs(T, 256, V, dtype, T + V, keep=0.9 if T < 1000 else 0.05)
+    _check(E.Loss(x, w, y, dw=T < 1000).run(), y)
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("T,V", [(5, 1000), (5, 9001), (200, 1000), (300, 40001)])
 def test_logits_of_minus_infinity(T, V, dtype):
