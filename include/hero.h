@@ -679,9 +679,10 @@ typedef struct hero_lm_loss_out {
   void *dx, *dw;
 } hero_lm_loss_out;
 
-/* Workspace bytes for hero_lm_loss with and without the two gradients (nonzero: wanted).  Host-only.  About
- * 0.5 GiB for the exponentials of a piece and, with dx, 0.25 for sums; with dw 2 d bytes a token.  fp32 models: about
- * three times that, and the head rows of a piece (up to 1.5 GiB). */
+/* Workspace bytes for hero_lm_loss with and without the two gradients (nonzero: wanted).  Host-only.  Few
+ * bytes a token; with a gradient up to 0.5 GiB for the exponentials of a piece and, with dx, 0.3 for sums; with dw 2 d bytes
+ * a token.  fp32 models from 128 tokens on: three bf16 terms of the exponentials and of the piece's head rows, up to 3.5
+ * GiB, and 6 d bytes a token, with dw 12 d. */
 int hero_lm_loss_workspace_size(const hero_dims *dims, int vocab, int T, int with_dx, int with_dw, size_t *bytes);
 
 /*

@@ -259,9 +259,10 @@ __global__ __launch_bounds__(512, 2) void lm_dw_part_kernel(ARows<bf16_t> A, BRo
 }
 
 // dW of few rows: little to compute and all of dW to write.  A workgroup takes 128 head rows, a wave 32 of them
-// (operand B: their g, held; bf16: two terms of it), and `width` columns of d (A: rows of x^T, staged in LDS, so that no load waits behind
-// a store: with both in one loop 26 rows of d = 3584 against 116669 took 303 us, so 162, 5.2 TB/s).  Rows of A are dealt out so that a lane's sixteen results are neighbours, and the four lanes of a head
-// row write 64 elements of it in whole lines.  G: groups of 32 (bf16) or 16 (fp32) tokens.
+// (operand B: their g, held; bf16: two terms of it), and `width` columns of d (A: rows of x^T, staged in LDS, so that
+// no load waits behind a store: with both in one loop 26 rows of d = 3584 against 116669 took 303 us, so 162, 5.2 TB/s).
+// Rows of A are dealt out so that a lane's sixteen results are neighbours, and the four lanes of a head row write 64
+// elements of it in whole lines.  G: groups of 32 (bf16) or 16 (fp32) tokens.
 template <typename T, int G>
 __global__ __launch_bounds__(256) void lm_dw_few(LmRows a, int cols, const T* __restrict__ g, const T* __restrict__ xT,
                                                  int pitch, int width, T* __restrict__ dw) {
@@ -597,9 +598,8 @@ hipError_t lm_dw(const LmRows& a, int v0, int cols, const void* g, const void* x
 // exponentiate (134 rows of d = 1536 against 1066 columns: 42 -> 31 us a call).  Few rows against a head of up to
 // 160 MB: the streaming form (3 rows of d = 768 against 77287 columns 43 -> 34 us a call, 8 of 2048 against 9000
 // 48 -> 37); larger heads draw 5.6 TB/s on the large tiles and 4.8 there (16 rows of 4096 against 128256: 185 and 222 us).
-// Longer rows gain nothing from slices:
-// 10 rows of d = 2048 against 39058 columns, 153 tiles, took 56 us so and 65 + 7 in five slices.  kLmF32: kept, or for few
-// rows the streaming form (28 rows of d = 3840 against 75583 columns 462 -> 256 us a call, 4.6 TB/s; 60 of 1024 against
+// Longer rows gain nothing from slices: 10 rows of d = 2048 against 39058 columns, 153 tiles, took 56 us so and 65 + 7
+// in five slices.  kLmF32: kept, or for few rows the streaming form (28 rows of d = 3840 against 75583 columns 462 -> 256 us a call, 4.6 TB/s; 60 of 1024 against
 // 30000 82 -> 54) where its workgroups take most CUs (64 of them: one row of 4096 against 8192 45 -> 67).
 LmParts lm_parts(int mode, int rows, int cols, int d) {
   const LmParts few{(cols + 127) / 128, 7, 0};

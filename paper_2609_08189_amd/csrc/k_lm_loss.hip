@@ -29,8 +29,8 @@ constexpr int kRowsThreads = 1024;
 // Tile height and K slices of the dx products of M rows, by one wave, a candidate a lane and turn: the time in
 // rounds of workgroups over the CUs, a round weighted by its height (as phase_rows) and by its k-tiles, of which
 // storing an fp32 tile takes about twelve, and the finishing pass's reading of all slices at 4 TB/s, at least 0.15 us
-// each (125 is a k-tile of 256 rows, 1.45 us).  2048 rows of d = 4096 against 32768 columns: 128-row tiles in one round 443 us, 256-row tiles in
-// two slices 399.
+// each (125 is a k-tile of 256 rows, 1.45 us).  2048 rows of d = 4096 against 32768 columns: 128-row tiles in one
+// round 443 us, 256-row tiles in two slices 399.
 __device__ __forceinline__ int dx_plan(const LmRows& a, int M, int lane) {
   float time = 3.0e38f;
   int best = 256 | 1 << 16;
@@ -597,8 +597,8 @@ __global__ __launch_bounds__(256) void lm_g_of_e_kernel(LmRows a, LmPiece p, voi
   if (b < nx)
     xT_tile<MODE>(tile, a, xT, pitch, b * 64, blockIdx.y * 64);
   else
-    g_tile<MODE, true, TWO>(tile, a, 0, p.cols, p.e, p.pitch, static_cast<size_t>(p.rows_max) * p.pitch, g, pitch, (b - nx) * 64,
-                       blockIdx.y * 64);
+    g_tile<MODE, true, TWO>(tile, a, 0, p.cols, p.e, p.pitch, static_cast<size_t>(p.rows_max) * p.pitch, g, pitch,
+                            (b - nx) * 64, blockIdx.y * 64);
 }
 
 // w_t[i][v] = w[v][i], zero from the vocabulary to the pitch (a multiple of 64)
