@@ -1986,13 +1986,22 @@ int hero_lm_loss(const hero_dims* dims, int vocab, int T, const void* x, const h
   a.xs = ws + L.xs;
   const bool mfma = L.mode != hero::kLmF32, split = L.mode == hero::kLmSplit;
   const float* wf = static_cast<const float*>(head->w);
+  hero::LmPiece p{};
+  const hero::LmParts form = hero::lm_parts(L.mode, L.chunk, vocab, D.d);
+  if (!dx && !dw && L.single && form.slices == 0 && form.shift == 7) {
+    p.cols = vocab;
+    p.part = reinterpret_cast<float2*>(ws + L.part);
+    p.parts = form.parts;
+    hipError_t y = timed(HERO_K_LM_LOGITS, s, [&] { return hero::launch_lm_score_logits(a, p, s); });
+    if (y == hipSuccess) y = timed(HERO_K_LM_COMBINE, s, [&] { return hero::launch_lm_score(a, p, s); });
+    return y == hipSuccess ? HERO_OK : HERO_E_LAUNCH;
+  }
   hipError_t e = timed(HERO_K_LM_ROWS, s, [&] {
     const hipError_t y = hero::launch_lm_rows(a, s);
     return y == hipSuccess && split
                ? hero::launch_lm_terms(static_cast<const float*>(x), D.d, a.idx, a.counts, T, D.d, a.xs, s)
                : y;
   });
-  hero::LmPiece p{};
   for (int c = 0; c < L.n_chunks && e == hipSuccess; ++c) {
     p.chunk = c;
     p.m0 = c * L.chunk;

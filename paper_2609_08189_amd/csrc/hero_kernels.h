@@ -466,6 +466,10 @@ struct LmParts {
 };
 LmParts lm_parts(int mode, int rows, int cols, int d);
 hipError_t launch_lm_logits(const LmRows& a, const LmPiece& p, hipStream_t s);
+// Loss without gradients of few tokens against a head of one piece, which streams past them (lm_parts: shift 7): the parts
+// of all tokens, then their losses; nothing else of a call
+hipError_t launch_lm_score_logits(const LmRows& a, const LmPiece& p, hipStream_t s);
+hipError_t launch_lm_score(const LmRows& a, const LmPiece& p, hipStream_t s);
 // the row's sums with this piece's; e in units of the row's reference after it; after the last piece its loss
 hipError_t launch_lm_combine(const LmRows& a, const LmPiece& p, hipStream_t s);
 hipError_t launch_lm_dx(const LmRows& a, const LmPiece& p, const void* w_t, int ld_wt, hipStream_t s);

@@ -411,14 +411,17 @@ struct FewRing {
   }
 };
 
-template <typename T, int TB, int NS, bool STORE>
+// SCORE: no exponential is kept, so a part may take its own maximum as reference, and neither the rows nor their targets'
+// logits are needed before: all tokens are rows (the head's passage costs the same), and one launch less comes first.
+template <typename T, int TB, int NS, bool STORE, bool SCORE = false>
 __global__ __launch_bounds__(256) void lm_logits_few(LmRows a, LmPiece p) {
   typedef FewRing<T, TB, NS> R;
   constexpr bool F32 = R::F32;
   constexpr int BX = R::BX;
   __shared__ __attribute__((aligned(1024))) unsigned char smem[NS * R::STAGE];
-  const int M = *p.count;
+  const int M = SCORE ? a.T : *p.count;
   if (M == 0) return;
+  if (SCORE && blockIdx.x == 0 && threadIdx.x == 0) *a.done = 0;
   const int lane = threadIdx.x & 63, l15 = lane & 15, q = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) >> 6);
   const int v0 = blockIdx.x * R::BV;
@@ -426,7 +429,10 @@ __global__ __launch_bounds__(256) void lm_logits_few(LmRows a, LmPiece p) {
   f32x4 acc[2][TB];
   R::run(static_cast<const unsigned char*>(a.w) + static_cast<size_t>(p.v0 + v0) * row_bytes, row_bytes, p.cols - v0,
          static_cast<const unsigned char*>(a.x),
-         [&](int r) { return static_cast<uint32_t>(a.idx[p.m0 + min(r, M - 1)]) * static_cast<uint32_t>(row_bytes); },
+         [&](int r) {
+           const int m = min(r, M - 1);
+           return static_cast<uint32_t>(SCORE ? m : a.idx[p.m0 + m]) * static_cast<uint32_t>(row_bytes);
+         },
          static_cast<int>(row_bytes / ROWB), smem, acc);   // d >= 256, fp32 128: four k-tiles at least
   static_assert(NS <= 5, "the first loads are of tiles that exist");
   // every wave is past its last reads; the ring's memory holds the columns' maxima and sums now
@@ -452,10 +458,15 @@ __global__ __launch_bounds__(256) void lm_logits_few(LmRows a, LmPiece p) {
 #pragma unroll
   for (int b = 0; b < TB; ++b) {
     const int m = 16 * b + l15, mc = p.m0 + min(m, M - 1);
-    const float r0 = a.ref[mc];
     const float t = fmaxf(fmaxf(top[m], top[BX + m]), fmaxf(top[2 * BX + m], top[3 * BX + m]));
-    ref[b] = t - r0 > kLmAbove ? t : r0;
-    const int tgt = a.tgt[mc] - p.v0 - n0;
+    if constexpr (SCORE) {
+      ref[b] = t == -INFINITY ? 0.f : t;
+    } else {
+      const float r0 = a.ref[mc];
+      ref[b] = t - r0 > kLmAbove ? t : r0;
+    }
+    // of a token that does not count any value: its sums are not read
+    const int tgt = SCORE ? static_cast<int>(static_cast<unsigned>(a.targets[mc]) - static_cast<unsigned>(n0)) : a.tgt[mc] - p.v0 - n0;
     float s = 0.f;
 #pragma unroll
     for (int f = 0; f < 2; ++f) {
@@ -599,8 +610,9 @@ hipError_t lm_dw(const LmRows& a, int v0, int cols, const void* g, const void* x
 // 160 MB: the streaming form (3 rows of d = 768 against 77287 columns 43 -> 34 us a call, 8 of 2048 against 9000
 // 48 -> 37); larger heads draw 5.6 TB/s on the large tiles and 4.8 there (16 rows of 4096 against 128256: 185 and 222 us).
 // Longer rows gain nothing from slices: 10 rows of d = 2048 against 39058 columns, 153 tiles, took 56 us so and 65 + 7
-// in five slices.  kLmF32: kept, or for few rows the streaming form (28 rows of d = 3840 against 75583 columns 462 -> 256 us a call, 4.6 TB/s; 60 of 1024 against
-// 30000 82 -> 54) where its workgroups take most CUs (64 of them: one row of 4096 against 8192 45 -> 67).
+// in five slices.  kLmF32: kept, or for few rows the streaming form (28 rows of d = 3840 against 75583 columns 462 ->
+// 256 us a call, 4.6 TB/s; 60 of 1024 against 30000 82 -> 54) where its workgroups take most CUs (64 of them: one row of
+// 4096 against 8192 45 -> 67).
 LmParts lm_parts(int mode, int rows, int cols, int d) {
   const LmParts few{(cols + 127) / 128, 7, 0};
   if (mode == kLmF32) {
@@ -612,6 +624,24 @@ LmParts lm_parts(int mode, int rows, int cols, int d) {
   if (S > 1) return {0, 0, S};
   if (mode == kLmBf16 && rows <= kLmFewRows && static_cast<long long>(cols) * d <= kLmFewHead) return few;
   return {4 * lm_tiles(cols), 0, 0};
+}
+
+hipError_t launch_lm_score_logits(const LmRows& a, const LmPiece& p, hipStream_t s) {
+  const int grid = (p.cols + 127) / 128;
+#define HERO_LM_SCORE(TYPE)                                                \
+  if (a.T <= 16)                                                        \
+    lm_logits_few<TYPE, 1, 4, false, true><<<grid, 256, 0, s>>>(a, p);     \
+  else if (a.T <= 32)                                                   \
+    lm_logits_few<TYPE, 2, 4, false, true><<<grid, 256, 0, s>>>(a, p);     \
+  else                                                                  \
+    lm_logits_few<TYPE, 4, 3, false, true><<<grid, 256, 0, s>>>(a, p)
+  if (a.mode == kLmBf16) {
+    HERO_LM_SCORE(bf16_t);
+  } else {
+    HERO_LM_SCORE(float);
+  }
+#undef HERO_LM_SCORE
+  return hipGetLastError();
 }
 
 hipError_t launch_lm_logits(const LmRows& a, const LmPiece& p, hipStream_t s) {

@@ -261,6 +261,97 @@ def test_last_pieces_that_would_be_narrow(T, V, dtype):
     _check(E.Loss(x, w, y, dw=T < 1000).run(), y)
 
 
+def _scored(x, w, y, **kw):
+    """The loss without gradients, checked."""
+    from tests import train_ends as E
+    c = E.Loss(x, w, y, dx=False, dw=False, **kw).run()
+    _check(c, y)
+    return c
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("T,d,V", [(1, 256, 16384), (1, 768, 20011), (2, 256, 14337), (16, 512, 30001), (17, 256, 33000), (32, 256, 14400),
+                                   (33, 512, 16001), (64, 1024, 20000), (64, 256, 131071), (5, 256, 131200)])
+def test_scoring_few_tokens(T, d, V, dtype):
+    import torch
+    from tests import train_ends as E
+    print(f"case lm_loss score T={T} d={d} V={V} {dtype}", flush=True)
+    x, w, y = _inputs(T, d, V, dtype, T + V, keep=1.0 if T < 4 else 0.7)
+    y[0] = V - 1
+    a, b = _scored(x, w, y, mean=T % 2 == 1, scale=0.7), _scored(x, w, y, mean=T % 2 == 1, scale=0.7)
+    assert all(torch.equal(a.out[k].t, b.out[k].t) for k in a.out)      # one order of every sum
+    far = x * 40
+    _scored(far, w, y)
+    sure = E.f64(w)[y] * 30 * (np.arange(T) % 2 == 0)[:, None]
+    _scored(x + torch.from_numpy(sure).to(x), w, y, mean=False)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_scoring_tokens_that_do_not_count_and_values_that_are_not_finite(dtype):
+    import torch
+    from tests import train_ends as E
+    print(f"case lm_loss score specials {dtype}", flush=True)
+    T, V = 40, 20011
+    x, w, y = _inputs(T, 256, V, dtype, 9, keep=1.0)
+    y[::3], y[1::9], y[5], y[8] = -100, V, 2 ** 31 - 1, -2 ** 31
+    dead = torch.from_numpy((y < 0) | (y >= V)).to(E.DEV)
+    clean = _scored(torch.where(dead[:, None], torch.zeros_like(x), x), w, y)
+    x[::3], x[1::9] = float("nan"), float("inf")
+    c = E.Loss(x, w, y, dx=False, dw=False).run()
+    for k, v in c.results().items():
+        assert np.array_equal(v, E.f64(clean.out[k].t)), k
+    assert not c.out["token_loss"].t[dead].any()
+    for mean in (True, False):
+        none = E.Loss(x, w, np.full(T, -1), dx=False, dw=False, mean=mean).run().results()
+        assert all(not v.any() for v in none.values())
+    # one counted row of NaN, one with an infinite element: no finite loss of these, the others as they were
+    x, w, y = _inputs(T, 256, V, dtype, 9, keep=1.0)
+    good = E.Loss(x, w, y, dx=False, dw=False).run().results()["token_loss"]
+    x[3], x[7, 5] = float("nan"), float("inf")
+    bad = E.Loss(x, w, y, dx=False, dw=False).run()
+    torch.cuda.synchronize()
+    token = E.f64(bad.out["token_loss"].t)
+    assert not np.isfinite(token[[3, 7]]).any() and not np.isfinite(float(bad.out["loss"].t))
+    keep = np.delete(np.arange(T), [3, 7])
+    assert np.array_equal(token[keep], good[keep])
+    # 128 columns of -infinity (a whole part), and one in each of the others, change nothing but their own share
+    x, w, y = _inputs(T, 256, V, dtype, 9, keep=1.0, sure=0.0)
+    x.abs_()
+    y = y % 128
+    gone = np.concatenate([np.arange(1280, 1408), np.arange(200, V, 128)])
+    w[torch.from_numpy(gone).to(E.DEV)] = -3e38
+    c = E.Loss(x, w, y, dx=False, dw=False).run()
+    rest = torch.ones(V, dtype=torch.bool, device=E.DEV)
+    rest[torch.from_numpy(gone).to(E.DEV)] = False
+    short = w[rest].contiguous()
+    E.check_loss(c, O.lm_loss(E.f64(x), E.f64(short), y), E.loss_bounds(E.f64(x), E.f64(short), y, 1.0, True, dtype))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_scoring_replays(dtype):
+    import torch
+    from tests import train_ends as E
+    print(f"case lm_loss score graph {dtype}", flush=True)
+    x, w, y = _inputs(20, 256, 20011, dtype, 3, keep=1.0)
+    c = E.Loss(x, w, y, dx=False, dw=False).run()
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        c.run()
+    for keep in (1.0, 0.3, 0.0, 0.8):
+        x2, _, y2 = _inputs(20, 256, 20011, dtype, 50 + int(10 * keep), keep=keep)
+        c.x.copy_(x2)
+        c.y.copy_(torch.as_tensor(y2, dtype=torch.int32))
+        eager = E.Loss(x2, w, y2, dx=False, dw=False).run()
+        for v in c.out.values():
+            v.poison()
+        torch.cuda.synchronize()
+        g.replay()
+        torch.cuda.synchronize()
+        for k, v in c.results().items():
+            assert np.array_equal(v, E.f64(eager.out[k].t)), k
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("T,V", [(5, 1000), (5, 9001), (200, 1000), (300, 40001)])
 def test_logits_of_minus_infinity(T, V, dtype):
