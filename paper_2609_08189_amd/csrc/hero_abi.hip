@@ -1714,8 +1714,8 @@ constexpr int kLmHeadRows = 1 << 17;         // head rows of a product, which ad
 
 // fp32 models: from so many tokens on the products of three-term operands are faster than those on the fp32 matrix
 // cores, which read operands without LDS: the head's terms cost a pass over it (4 bytes read, 6 written an
-// element), a row 2 d operations at 75 against 230 TFLOP/s.  With dx, d = 1024, 30000 columns: 64 tokens 281 us so, 153
-// in fp32; 127 tokens 304 and 249; 255 tokens 341 and 436; 500 tokens with dW too 667 and 1333.  192 tokens of
+// element), a row 2 d operations at 75 against 230 TFLOP/s (128 tokens and fewer stream: 115).  With dx and dW, d = 1024,
+// 30000 columns: 127 tokens 334 us in fp32; 130 tokens 447 so and 731 in fp32, 256 tokens 517 and 752.  192 tokens of
 // d = 2304 against 45397 without gradients 499 and 644; 300 of 256 against 5000 with both 101 and 90.
 constexpr int kLmSplitRows = 128;
 
@@ -1989,7 +1989,7 @@ int hero_lm_loss(const hero_dims* dims, int vocab, int T, const void* x, const h
   const float* wf = static_cast<const float*>(head->w);
   hero::LmPiece p{};
   const hero::LmParts form = hero::lm_parts(L.mode, L.chunk, vocab, D.d);
-  if (!dx && !dw && L.single && form.slices == 0 && form.shift == 7) {
+  if (!dx && !dw && L.single && T <= hero::kLmFewRows && form.slices == 0 && form.shift == 7) {
     p.cols = vocab;
     p.part = reinterpret_cast<float2*>(ws + L.part);
     p.parts = form.parts;

@@ -458,6 +458,7 @@ struct LmPiece {
 constexpr int kLmLogitsMax = 8192;   // columns of a piece whose logits are kept (kLmF32: of any)
 constexpr int kLmFewRows = 64;       // bf16 rows that the head streams past at once,
 constexpr long long kLmFewHead = 80000000;   // and elements of such a head
+constexpr int kLmFewRowsF32 = 128;   // ... and fp32 rows, most heads
 constexpr int kLmFewF32 = 112;       // fp32 rows do so from so many columns in 128s on,
 constexpr long long kLmFewDx = 12000000;     // and W^T past the rows of e from so many elements
 // which of the forms the logits take: parts and shift of a row (slices 0), or K slices of kept logits

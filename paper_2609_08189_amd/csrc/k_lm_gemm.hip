@@ -338,7 +338,7 @@ template <typename T, int TB, int NS>
 struct FewRing {
   static constexpr bool F32 = std::is_same_v<T, float>;
   static constexpr int BV = 128, BX = 16 * TB, STAGE = (BV + BX) * ROWB;
-  static constexpr int XL = TB < 4 ? 1 : 2;        // loads a wave of x (TB 1: two waves repeat the others')
+  static constexpr int XL = TB < 4 ? 1 : TB / 2;   // loads a wave of x (TB 1: two waves repeat the others')
   static constexpr int L = 4 + XL;
   typedef std::conditional_t<F32, f32x4, bf16x8> Frag;
   // acc[f][b]: rows 16 f of the wave's 32 of w (`rows` of them, the last repeated), rows 16 b of x; w and x at k-tile 0 of
@@ -613,10 +613,15 @@ hipError_t lm_dw(const LmRows& a, int v0, int cols, const void* g, const void* x
 // in five slices.  kLmF32: kept, or for few rows the streaming form (28 rows of d = 3840 against 75583 columns 462 ->
 // 256 us a call, 4.6 TB/s; 60 of 1024 against 30000 82 -> 54) where its workgroups take most CUs (64 of them: one row of
 // 4096 against 8192 45 -> 67).
+// fp32 rows that the head, or W^T, streams past: with more than 64 one workgroup fills a CU's LDS, and narrow heads pay
+// for its ends (96 rows of d = 1024 against 30000 columns, logits and dx, 327 -> 178 us a call, 127 of 2304 against 45397
+// 447 -> 336 the logits; 127 of 512 against 16000 48 and 53).
+static bool lm_f32_few(int rows, int d) { return rows <= kLmFewRows || (rows <= kLmFewRowsF32 && d >= 1024); }
+
 LmParts lm_parts(int mode, int rows, int cols, int d) {
   const LmParts few{(cols + 127) / 128, 7, 0};
   if (mode == kLmF32) {
-    if (rows <= kLmFewRows && (cols + 127) / 128 >= kLmFewF32) return few;
+    if (lm_f32_few(rows, d) && (cols + 127) / 128 >= kLmFewF32) return few;
     return cols <= kLmLogitsMax ? LmParts{0, 0, 1} : LmParts{(cols + 8191) / 8192, 13, 1};
   }
   const int tiles = (rows + 127) / 128 * lm_tiles(cols), ktiles = d / 64 * (mode == kLmSplit ? 6 : 1);
@@ -655,12 +660,16 @@ hipError_t launch_lm_logits(const LmRows& a, const LmPiece& p, hipStream_t s) {
     HERO_LM_FEW(T, 1, 4);        \
   else if (p.rows_max <= 32)     \
     HERO_LM_FEW(T, 2, 4);        \
-  else                           \
+  else if (p.rows_max <= 64)     \
     HERO_LM_FEW(T, 4, 3)
     if (a.mode == kLmBf16) {
       HERO_LM_FEW_ROWS(bf16_t);
     } else {
       HERO_LM_FEW_ROWS(float);
+      else if (p.rows_max <= 96)
+        HERO_LM_FEW(float, 6, 3);
+      else
+        HERO_LM_FEW(float, 8, 3);
     }
 #undef HERO_LM_FEW_ROWS
 #undef HERO_LM_FEW
@@ -676,7 +685,7 @@ hipError_t launch_lm_logits(const LmRows& a, const LmPiece& p, hipStream_t s) {
 // read 64-byte pieces of rows (60 rows of d = 4096 against 128256 columns with the logits 1759 -> 1175 us a call, 60 of 256
 // against 100000 176 -> 130; against 10000 of d = 1024 80 and 83)
 int lm_f32_few_slices(int rows, int d, int K) {
-  if (rows > kLmFewRows || K < 256 || static_cast<long long>(d) * K < kLmFewDx) return 0;
+  if (!lm_f32_few(rows, d) || K < 256 || static_cast<long long>(d) * K < kLmFewDx) return 0;
   return std::max(1, std::min({2 * kCUs / (d / 128), K / 256, 64}));
 }
 
@@ -690,8 +699,12 @@ hipError_t launch_lm_dx(const LmRows& a, const LmPiece& p, const void* w_t, int 
       lm_f32_dx_few<1, 4><<<grid, 256, 0, s>>>(a, p, wt, ld_wt, a.f32_slices);
     else if (p.rows_max <= 32)
       lm_f32_dx_few<2, 4><<<grid, 256, 0, s>>>(a, p, wt, ld_wt, a.f32_slices);
-    else
+    else if (p.rows_max <= 64)
       lm_f32_dx_few<4, 3><<<grid, 256, 0, s>>>(a, p, wt, ld_wt, a.f32_slices);
+    else if (p.rows_max <= 96)
+      lm_f32_dx_few<6, 3><<<grid, 256, 0, s>>>(a, p, wt, ld_wt, a.f32_slices);
+    else
+      lm_f32_dx_few<8, 3><<<grid, 256, 0, s>>>(a, p, wt, ld_wt, a.f32_slices);
     return hipGetLastError();
   }
   return launch_lm_f32_dx(static_cast<const float*>(p.e), p.count, p.rows_max, p.pitch, static_cast<const float*>(w_t) + p.v0,

@@ -244,7 +244,8 @@ def test_two_calls_on_two_streams():
 
 
 @pytest.mark.parametrize("T,d,V,size", [(1, 512, 30000, 1.0), (16, 1024, 15001, 1.0), (17, 640, 33003, 1.0), (33, 512, 30001, 1.0),
-                                        (64, 1024, 16000, 1.0), (20, 512, 30000, 120.0), (50, 256, 140001, 60.0), (3, 128, 131073, 1.0)])
+                                        (64, 1024, 16000, 1.0), (65, 1024, 15000, 1.0), (96, 1024, 14401, 60.0), (97, 1152, 16001, 1.0),
+                                        (127, 1024, 15003, 120.0), (128, 1152, 15003, 1.0), (20, 512, 30000, 120.0), (50, 256, 140001, 60.0), (3, 128, 131073, 1.0)])
 def test_few_fp32_rows_against_large_heads(T, d, V, size):
     from tests import train_ends as E
     print(f"case lm_loss few fp32 rows T={T} d={d} V={V} size={size}", flush=True)
