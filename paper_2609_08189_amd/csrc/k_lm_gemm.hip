@@ -264,12 +264,11 @@ __global__ __launch_bounds__(512, 2) void lm_dw_part_kernel(ARows<bf16_t> A, BRo
 // Rows of A are dealt out so that a lane's sixteen results are neighbours, and the four lanes of a head row write 64
 // elements of it in whole lines.  G: groups of 32 (bf16) or 16 (fp32) tokens.
 template <typename T, int G>
-__global__ __launch_bounds__(256) void lm_dw_few(LmRows a, int cols, const T* __restrict__ g, const T* __restrict__ xT,
-                                                 int pitch, int width, T* __restrict__ dw) {
+__device__ __forceinline__ void dw_few(const LmRows& a, int cols, const T* __restrict__ g, const T* __restrict__ xT, int pitch,
+                                       int width, T* __restrict__ dw, unsigned char* xs) {
   constexpr bool F32 = std::is_same_v<T, float>;
   typedef std::conditional_t<F32, f32x4, bf16x8> Frag;
   constexpr int E = F32 ? 4 : 8, ROW = 64 * G + 16;   // bytes of a staged row: 16-byte reads of 16 rows miss each other
-  __shared__ __attribute__((aligned(16))) unsigned char xs[(G <= 4 ? 256 : 128) * ROW];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l15 = lane & 15, q = lane >> 4;
   const int i0 = blockIdx.y * width, di = min(width, a.d - i0);
   for (int e = threadIdx.x; e < di * 4 * G; e += 256)
@@ -324,6 +323,21 @@ __global__ __launch_bounds__(256) void lm_dw_few(LmRows a, int cols, const T* __
       }
     }
   }
+}
+
+// as many groups as the counted tokens fill, of the MOST that the call may have
+template <typename T, int MOST>
+__global__ __launch_bounds__(256) void lm_dw_few(LmRows a, int cols, const T* __restrict__ g, const T* __restrict__ xT,
+                                                 int pitch, int width, T* __restrict__ dw) {
+  constexpr int GROUP = std::is_same_v<T, float> ? 16 : 32;
+  __shared__ __attribute__((aligned(16))) unsigned char xs[(MOST <= 4 ? 256 : 128) * (64 * MOST + 16)];
+  const int N = a.counts[0];
+  if (MOST == 1 || N <= GROUP) return dw_few<T, 1>(a, cols, g, xT, pitch, width, dw, xs);
+  if constexpr (MOST >= 2)
+    if (MOST == 2 || N <= 2 * GROUP) return dw_few<T, 2>(a, cols, g, xT, pitch, width, dw, xs);
+  if constexpr (MOST >= 4)
+    if (MOST == 4 || N <= 4 * GROUP) return dw_few<T, 4>(a, cols, g, xT, pitch, width, dw, xs);
+  if constexpr (MOST >= 8) dw_few<T, 8>(a, cols, g, xT, pitch, width, dw, xs);
 }
 
 // ---------------------------------------------------------------------------
@@ -413,15 +427,11 @@ struct FewRing {
 
 // SCORE: no exponential is kept, so a part may take its own maximum as reference, and neither the rows nor their targets'
 // logits are needed before: all tokens are rows (the head's passage costs the same), and one launch less comes first.
-template <typename T, int TB, int NS, bool STORE, bool SCORE = false>
-__global__ __launch_bounds__(256) void lm_logits_few(LmRows a, LmPiece p) {
+template <typename T, int TB, int NS, bool STORE, bool SCORE>
+__device__ __forceinline__ void few_logits(const LmRows& a, const LmPiece& p, int M, unsigned char* smem) {
   typedef FewRing<T, TB, NS> R;
   constexpr bool F32 = R::F32;
   constexpr int BX = R::BX;
-  __shared__ __attribute__((aligned(1024))) unsigned char smem[NS * R::STAGE];
-  const int M = SCORE ? a.T : *p.count;
-  if (M == 0) return;
-  if (SCORE && blockIdx.x == 0 && threadIdx.x == 0) *a.done = 0;
   const int lane = threadIdx.x & 63, l15 = lane & 15, q = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x) >> 6);
   const int v0 = blockIdx.x * R::BV;
@@ -502,13 +512,38 @@ __global__ __launch_bounds__(256) void lm_logits_few(LmRows a, LmPiece p) {
     }
 }
 
+// The ring's width by the rows that count, up to MOST blocks of 16 (the host's bound, which sizes the LDS): fp32 products of
+// all rows where 29 of 96 count: 894 us a call with both gradients, d = 2304 against 45397 columns, so 565.
+template <int MOST>
+constexpr int kFewBytes = MOST == 1 ? 4 * 144 * ROWB : MOST <= 4 ? 4 * 160 * ROWB : 3 * (128 + 16 * MOST) * ROWB;
+template <int N>
+using Int = std::integral_constant<int, N>;
+template <int MOST, class F>
+__device__ __forceinline__ void few_case(int M, F f) {
+  if (MOST == 1 || M <= 16) return f(Int<1>(), Int<4>());
+  if constexpr (MOST >= 2)
+    if (MOST == 2 || M <= 32) return f(Int<2>(), Int<4>());
+  if constexpr (MOST >= 4)
+    if (MOST == 4 || M <= 64) return f(Int<4>(), Int<3>());
+  if constexpr (MOST >= 6)
+    if (MOST == 6 || M <= 96) return f(Int<6>(), Int<3>());
+  if constexpr (MOST >= 8) f(Int<8>(), Int<3>());
+}
+
+template <typename T, int MOST, bool STORE, bool SCORE = false>
+__global__ __launch_bounds__(256) void lm_logits_few(LmRows a, LmPiece p) {
+  __shared__ __attribute__((aligned(1024))) unsigned char smem[kFewBytes<MOST>];
+  const int M = SCORE ? a.T : *p.count;
+  if (M == 0) return;
+  if (SCORE && blockIdx.x == 0 && threadIdx.x == 0) *a.done = 0;
+  few_case<MOST>(M, [&](auto tb, auto ns) { few_logits<T, decltype(tb)::value, decltype(ns)::value, STORE, SCORE>(a, p, M, smem); });
+}
+
 // dx of few fp32 rows the same way: W^T streams past the rows of e, slice z of K into acc + z M d
 template <int TB, int NS>
-__global__ __launch_bounds__(256) void lm_f32_dx_few(LmRows a, LmPiece p, const float* __restrict__ w_t, int ld_wt, int slices) {
+__device__ __forceinline__ void f32_dx_few(const LmRows& a, const LmPiece& p, const float* __restrict__ w_t, int ld_wt, int slices,
+                                           int M, unsigned char* smem) {
   typedef FewRing<float, TB, NS> R;
-  __shared__ __attribute__((aligned(1024))) unsigned char smem[NS * R::STAGE];
-  const int M = *p.count;
-  if (M == 0) return;
   const int lane = threadIdx.x & 63, l15 = lane & 15, q = lane >> 4, wave = threadIdx.x >> 6;
   const int i0 = blockIdx.x * R::BV, z = blockIdx.y, all = p.pitch * 4 / ROWB;
   const int k0 = static_cast<int>(static_cast<long long>(all) * z / slices);
@@ -528,6 +563,16 @@ __global__ __launch_bounds__(256) void lm_f32_dx_few(LmRows a, LmPiece p, const 
       *o = p.first ? acc[f][b] : a.alpha[p.m0 + m] * *o + acc[f][b];
     }
   }
+}
+
+template <int MOST>
+__global__ __launch_bounds__(256) void lm_f32_dx_few(LmRows a, LmPiece p, const float* __restrict__ w_t, int ld_wt, int slices) {
+  __shared__ __attribute__((aligned(1024))) unsigned char smem[kFewBytes<MOST>];
+  const int M = *p.count;
+  if (M == 0) return;
+  few_case<MOST>(M, [&](auto tb, auto ns) {
+    f32_dx_few<decltype(tb)::value, decltype(ns)::value>(a, p, w_t, ld_wt, slices, M, smem);
+  });
 }
 
 int lm_tiles(int n) { return (n + 255) / 256; }
@@ -635,11 +680,11 @@ hipError_t launch_lm_score_logits(const LmRows& a, const LmPiece& p, hipStream_t
   const int grid = (p.cols + 127) / 128;
 #define HERO_LM_SCORE(TYPE)                                                \
   if (a.T <= 16)                                                        \
-    lm_logits_few<TYPE, 1, 4, false, true><<<grid, 256, 0, s>>>(a, p);     \
+    lm_logits_few<TYPE, 1, false, true><<<grid, 256, 0, s>>>(a, p);     \
   else if (a.T <= 32)                                                   \
-    lm_logits_few<TYPE, 2, 4, false, true><<<grid, 256, 0, s>>>(a, p);     \
+    lm_logits_few<TYPE, 2, false, true><<<grid, 256, 0, s>>>(a, p);     \
   else                                                                  \
-    lm_logits_few<TYPE, 4, 3, false, true><<<grid, 256, 0, s>>>(a, p)
+    lm_logits_few<TYPE, 4, false, true><<<grid, 256, 0, s>>>(a, p)
   if (a.mode == kLmBf16) {
     HERO_LM_SCORE(bf16_t);
   } else {
@@ -652,24 +697,24 @@ hipError_t launch_lm_score_logits(const LmRows& a, const LmPiece& p, hipStream_t
 hipError_t launch_lm_logits(const LmRows& a, const LmPiece& p, hipStream_t s) {
   if (!p.logits && p.shift) {   // the streaming form
     const int grid = (p.cols + 127) / 128;
-#define HERO_LM_FEW(T, TB, NS)                                      \
-  (p.e ? lm_logits_few<T, TB, NS, true><<<grid, 256, 0, s>>>(a, p) \
-       : lm_logits_few<T, TB, NS, false><<<grid, 256, 0, s>>>(a, p))
+#define HERO_LM_FEW(T, MOST)                                      \
+  (p.e ? lm_logits_few<T, MOST, true><<<grid, 256, 0, s>>>(a, p) \
+       : lm_logits_few<T, MOST, false><<<grid, 256, 0, s>>>(a, p))
 #define HERO_LM_FEW_ROWS(T)      \
   if (p.rows_max <= 16)          \
-    HERO_LM_FEW(T, 1, 4);        \
+    HERO_LM_FEW(T, 1);        \
   else if (p.rows_max <= 32)     \
-    HERO_LM_FEW(T, 2, 4);        \
+    HERO_LM_FEW(T, 2);        \
   else if (p.rows_max <= 64)     \
-    HERO_LM_FEW(T, 4, 3)
+    HERO_LM_FEW(T, 4)
     if (a.mode == kLmBf16) {
       HERO_LM_FEW_ROWS(bf16_t);
     } else {
       HERO_LM_FEW_ROWS(float);
       else if (p.rows_max <= 96)
-        HERO_LM_FEW(float, 6, 3);
+        HERO_LM_FEW(float, 6);
       else
-        HERO_LM_FEW(float, 8, 3);
+        HERO_LM_FEW(float, 8);
     }
 #undef HERO_LM_FEW_ROWS
 #undef HERO_LM_FEW
@@ -696,15 +741,15 @@ hipError_t launch_lm_dx(const LmRows& a, const LmPiece& p, const void* w_t, int 
     const float* wt = static_cast<const float*>(w_t);
     const dim3 grid(a.d / 128, a.f32_slices);
     if (p.rows_max <= 16)
-      lm_f32_dx_few<1, 4><<<grid, 256, 0, s>>>(a, p, wt, ld_wt, a.f32_slices);
+      lm_f32_dx_few<1><<<grid, 256, 0, s>>>(a, p, wt, ld_wt, a.f32_slices);
     else if (p.rows_max <= 32)
-      lm_f32_dx_few<2, 4><<<grid, 256, 0, s>>>(a, p, wt, ld_wt, a.f32_slices);
+      lm_f32_dx_few<2><<<grid, 256, 0, s>>>(a, p, wt, ld_wt, a.f32_slices);
     else if (p.rows_max <= 64)
-      lm_f32_dx_few<4, 3><<<grid, 256, 0, s>>>(a, p, wt, ld_wt, a.f32_slices);
+      lm_f32_dx_few<4><<<grid, 256, 0, s>>>(a, p, wt, ld_wt, a.f32_slices);
     else if (p.rows_max <= 96)
-      lm_f32_dx_few<6, 3><<<grid, 256, 0, s>>>(a, p, wt, ld_wt, a.f32_slices);
+      lm_f32_dx_few<6><<<grid, 256, 0, s>>>(a, p, wt, ld_wt, a.f32_slices);
     else
-      lm_f32_dx_few<8, 3><<<grid, 256, 0, s>>>(a, p, wt, ld_wt, a.f32_slices);
+      lm_f32_dx_few<8><<<grid, 256, 0, s>>>(a, p, wt, ld_wt, a.f32_slices);
     return hipGetLastError();
   }
   return launch_lm_f32_dx(static_cast<const float*>(p.e), p.count, p.rows_max, p.pitch, static_cast<const float*>(w_t) + p.v0,
